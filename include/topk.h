@@ -52,8 +52,9 @@ enum {
     TK_ERR_INVALID = -1,  /* bad argument (range, NULL, alignment, size) */
     TK_ERR_ALLOC = -2,    /* workspace too small / allocation failed */
     TK_ERR_CUDA = -3,     /* a CUDA runtime call failed */
-    /* -4 is not used: no kernel of the library waits on a flag (all device-side waiting is a
-       cooperative-groups grid or cluster barrier), so there is no wait that could expire */
+    /* -4 is not used: no kernel of a step waits on a flag (all its device-side waiting is a
+       cooperative-groups grid or cluster barrier), so there is no wait that could expire; the
+       bounded waits of the training operators report TK_ERR_INTERNAL (tk_xent_status) */
     TK_ERR_INTERNAL = -5, /* a device-side consistency check failed */
     TK_ERR_TOO_LARGE = -6 /* the problem does not fit the built-in scratch of tk_topk_noalloc */
 };
@@ -386,6 +387,126 @@ void tk_destroy(tk_ctx* ctx);
 
 /* Free the scratch pool used by tk_topk and the tk_last_* calls. */
 void tk_release_scratch(void);
+
+/* ---------------------------------------------------------------------------------------------
+ * Training operators: what stands on either side of a compressed step.  The layer norm and the
+ * softmax cross entropy of a large vocabulary make the gradients whose rows tk_step takes; AdamW
+ * applies a (dense) message where plain w -= alpha * message is not the update wanted.
+ *
+ * They need no context: each call enqueues its kernels on cuda_stream (a cudaStream_t, NULL = the
+ * legacy default stream) and returns.  No call allocates, synchronises (except tk_xent_status) or
+ * keeps anything between calls; scratch memory is the caller's workspace, whose contents do not
+ * matter before and after a call, and which two calls may share if their work does not overlap.  They can be captured into a CUDA graph.
+ *
+ * Matrices are given by a pointer to their first value and a row stride in values (>= the row
+ * length); a row's values are contiguous.  Values are fp32 or bf16; all sums, statistics and states
+ * are fp32 (or wider in effect), rounded once on output.  Any alignment that suits the type is
+ * accepted; rows whose starts are multiples of 16 bytes are faster.  Results do not depend on
+ * timing: no floating-point atomics.
+ */
+enum { TK_F32 = 0, TK_BF16 = 1 };
+
+/*
+ * Layer norm of every row:  y = gain * (x - mean) * rstd + bias,  rstd = 1 / sqrt(var + eps), with
+ * var = sum (x - mean)^2 / dim.
+ *   x [rows][dim], x_type   rows >= 0, 1 <= dim <= 2^24; y has the same type
+ *   gain, bias [dim]        of param_type; bias may be NULL (none)
+ *   eps                     finite, >= 0
+ *   mean, rstd [rows]       receive the statistics the backward pass takes; both or neither NULL
+ * y may be x itself (same stride).
+ */
+int tk_layernorm_forward(const void* x_dev, int x_type, int64_t rows, int64_t dim, int64_t x_stride,
+                         const void* gain_dev, const void* bias_dev, int param_type, float eps,
+                         void* y_dev, int64_t y_stride, float* mean_dev, float* rstd_dev, void* cuda_stream);
+
+/*
+ * Its gradient:  with z = (x - mean) rstd and t = dy gain (products element by element),
+ *   dx = rstd (t - mean(t) - z mean(t z)),  dgain = sum over rows of dy z,  dbias = sum over rows of dy.
+ *   dy, x, dx           [rows][dim] of x_type
+ *   dgain, dbias [dim]  of grad_type; with rows = 0 they become zero
+ * Any of dx, dgain, dbias may be NULL (not wanted), not all three.  The workspace (16-byte aligned,
+ * tk_layernorm_workspace_bytes; 0 for invalid sizes) is needed unless dgain and dbias are both NULL.
+ * dx may be dy or x itself (same stride) if dgain and dbias are NULL or dim <= 4096.
+ */
+size_t tk_layernorm_workspace_bytes(int64_t rows, int64_t dim);
+int tk_layernorm_backward(const void* dy_dev, int64_t dy_stride, const void* x_dev, int64_t x_stride, int x_type,
+                          int64_t rows, int64_t dim, const void* gain_dev, int param_type,
+                          const float* mean_dev, const float* rstd_dev, void* dx_dev, int64_t dx_stride,
+                          void* dgain_dev, void* dbias_dev, int grad_type,
+                          void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Softmax cross entropy of a linear head, without ever holding the logits l = h w^T:
+ *   lse_i = log sum_v exp(l_iv),   loss_i = lse_i - l_i,target(i)
+ *   h [tokens][dim], w [vocab][dim]   of in_type; 0 <= tokens <= 2^24, 1 <= vocab <= 2^26, 1 <= dim <= 2^20
+ *   target [tokens]    int32.  A negative target takes no part: its loss is 0, its gradient too.
+ *                      One >= vocab is an error the host cannot see: its loss is NaN, its gradient 0.
+ *   loss, lse [tokens] fp32
+ * tk_xent_grad continues from lse, with dloss [tokens] (fp32) the gradient of what the losses went into:
+ *   D_iv = dloss_i (exp(l_iv - lse_i) - [v = target(i)]),   dh = D w,   dw = D^T h
+ *   dh [tokens][dim], dw [vocab][dim]   of grad_type; either may be NULL (not wanted), not both
+ * The vocabulary is taken in pieces; the logits of a piece are computed again and turned into that
+ * piece of D in the workspace.
+ * Types: bf16 inputs with bf16 or fp32 gradients, fp32 inputs with fp32 gradients.  bf16 gradients round
+ * D to bf16 for the two products (fp32 sums); fp32 gradients and fp32 inputs are computed to fp32
+ * accuracy, from three bf16 parts of each fp32 operand, at three to six times the arithmetic.
+ * Workspace: 256-byte aligned, tk_xent_workspace_bytes (0 for invalid sizes).  grad_type -1 there: for
+ * the loss only.  aligned_rows: 1 if h and w start on 16-byte boundaries and their strides are
+ * multiples of 8 values; otherwise (0) room for copies of them is added (fp32 inputs are always copied).
+ * The kernels wait on barriers of their own, for two seconds at most; tk_xent_status synchronises the device,
+ * returns TK_ERR_INTERNAL if such a wait has run out since it was last asked (the results of that call are
+ * then unusable) and TK_OK otherwise.
+ */
+size_t tk_xent_workspace_bytes(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type, int aligned_rows);
+int tk_xent_loss(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int in_type,
+                 int64_t tokens, int64_t vocab, int64_t dim, const int32_t* target_dev,
+                 float* loss_dev, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int tk_xent_grad(const void* h_dev, int64_t h_stride, const void* w_dev, int64_t w_stride, int in_type,
+                 int64_t tokens, int64_t vocab, int64_t dim, const int32_t* target_dev,
+                 const float* lse_dev, const float* dloss_dev, void* dh_dev, int64_t dh_stride,
+                 void* dw_dev, int64_t dw_stride, int grad_type,
+                 void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int tk_xent_status(void);
+
+/*
+ * One AdamW step over many tensors (decoupled weight decay, bias-corrected moments):
+ *   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2          g = grad_scale * gradient
+ *   p <- p - lr weight_decay p - lr / (1 - b1^step) * m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * One launch serves up to 500 tensors.  The arrays `tensors` and `grads` are host memory and may be
+ * reused as soon as the call returns.
+ *   n             values of the tensor, >= 0
+ *   param         [n] of param_type, updated in place
+ *   copy16        NULL, or [n] bf16 that receives the updated parameters rounded to bf16
+ *   m, v          states.  32 bits: [n] fp32.  8 bits: 256 * ceil(n / 256) bytes each, 8-byte aligned,
+ *                 and scales: 2 * ceil(n / 256) fp32, 8-byte aligned.  All zero bytes is the initial state.
+ *   grads[i]      [n] of grad_type, read only
+ * 8-bit states.  256 consecutive values of a tensor share one fp32 scale s per state.  m is held as
+ * +-c^2 s, c = 0 .. 127, s = max|m| / 127^2; of v its root is held, sqrt(v) = c^2 s, c = 0 .. 255,
+ * s = max sqrt(v) / 255^2; c is the code of the nearest value (at least 1 for a positive v).  A
+ * block whose s would be below the smallest normal number holds zeros.  The order of the bytes within a
+ * block is the library's own: tk_adamw_get_state writes the values they stand for (m[i], v[i]: [n]
+ * fp32), tk_adamw_set_state is the reverse (checkpoints; states in 8 bits only, param and grads unused).
+ */
+typedef struct tk_adamw_tensor {
+    int64_t n;
+    void* param;
+    void* copy16;
+    void* m;
+    void* v;
+    float* scales;
+    double weight_decay;
+} tk_adamw_tensor;
+typedef struct tk_adamw_options {
+    double lr, beta1, beta2, eps, grad_scale;   /* finite; 0 <= beta < 1; eps >= 0 */
+    int64_t step;                               /* >= 1: the number of this step */
+    int32_t param_type, grad_type, state_bits;  /* TK_F32 / TK_BF16; 8 or 32 */
+} tk_adamw_options;
+int tk_adamw_step(const tk_adamw_tensor* tensors, const void* const* grads, int32_t count,
+                  const tk_adamw_options* options, void* cuda_stream);
+int tk_adamw_set_state(const tk_adamw_tensor* tensors, const float* const* m_dev, const float* const* v_dev,
+                       int32_t count, void* cuda_stream);
+int tk_adamw_get_state(const tk_adamw_tensor* tensors, float* const* m_dev, float* const* v_dev,
+                       int32_t count, void* cuda_stream);
 
 const char* tk_strerror(int code);
 

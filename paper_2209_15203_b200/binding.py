@@ -23,7 +23,13 @@ TK_MODE_EF = 2
 EXPORTS = ["tk_workspace_bytes", "tk_init", "tk_step", "tk_step_uplink", "tk_messages", "tk_step_server", "tk_step_host", "tk_topk", "tk_topk_noalloc", "tk_topk_noalloc_status", "tk_ef_bytes",
            "tk_ef_attach", "tk_ef_state", "tk_set_diagnostics", "tk_diagnostics", "tk_set_kdown",
            "tk_last_uplink", "tk_last_aggregate", "tk_last_downlink", "tk_status", "tk_set_profile",
-           "tk_set_force_general", "tk_set_cand_cap", "tk_set_bound_reuse", "tk_comm_model", "tk_set_graph", "tk_launch_count", "tk_debug_phase_clock", "tk_destroy", "tk_release_scratch", "tk_strerror"]
+           "tk_set_force_general", "tk_set_cand_cap", "tk_set_bound_reuse", "tk_comm_model", "tk_set_graph", "tk_launch_count", "tk_debug_phase_clock", "tk_destroy", "tk_release_scratch", "tk_strerror",
+           "tk_layernorm_forward", "tk_layernorm_workspace_bytes", "tk_layernorm_backward",
+           "tk_xent_workspace_bytes", "tk_xent_loss", "tk_xent_grad", "tk_xent_status",
+           "tk_adamw_step", "tk_adamw_set_state", "tk_adamw_get_state"]
+
+TK_F32 = 0
+TK_BF16 = 1
 
 
 class TkError(RuntimeError):
@@ -50,6 +56,17 @@ class tk_comm(ctypes.Structure):
                 ("downlink_words_uni", ctypes.c_int64), ("downlink_words_bi", ctypes.c_int64),
                 ("time_uni", ctypes.c_double), ("time_uni_union", ctypes.c_double), ("time_bi", ctypes.c_double),
                 ("compression_factor", ctypes.c_double)]
+
+
+class tk_adamw_tensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param", ctypes.c_void_p), ("copy16", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("weight_decay", ctypes.c_double)]
+
+
+class tk_adamw_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("step", ctypes.c_int64), ("param_type", ctypes.c_int32),
+                ("grad_type", ctypes.c_int32), ("state_bits", ctypes.c_int32)]
 
 
 _lib = None
@@ -126,6 +143,22 @@ def load(build_if_missing: bool = True):
     lib.tk_release_scratch.restype = None
     lib.tk_strerror.argtypes = [ctypes.c_int]
     lib.tk_strerror.restype = ctypes.c_char_p
+    size, cint = ctypes.c_size_t, ctypes.c_int
+    lib.tk_layernorm_forward.argtypes = [vp, cint, i64, i64, i64, vp, vp, cint, f32, vp, i64, vp, vp, vp]
+    lib.tk_layernorm_workspace_bytes.argtypes = [i64, i64]
+    lib.tk_layernorm_workspace_bytes.restype = size
+    lib.tk_layernorm_backward.argtypes = [vp, i64, vp, i64, cint, i64, i64, vp, cint, vp, vp, vp, i64, vp, vp, cint, vp, size, vp]
+    lib.tk_xent_workspace_bytes.argtypes = [i64, i64, i64, cint, cint, cint]
+    lib.tk_xent_workspace_bytes.restype = size
+    lib.tk_xent_loss.argtypes = [vp, i64, vp, i64, cint, i64, i64, i64, vp, vp, vp, vp, size, vp]
+    lib.tk_xent_grad.argtypes = [vp, i64, vp, i64, cint, i64, i64, i64, vp, vp, vp, vp, i64, vp, i64, cint, vp, size, vp]
+    lib.tk_xent_status.argtypes = []
+    lib.tk_adamw_step.argtypes = [vp, vp, i32, ctypes.POINTER(tk_adamw_options), vp]
+    lib.tk_adamw_set_state.argtypes = [vp, vp, vp, i32, vp]
+    lib.tk_adamw_get_state.argtypes = [vp, vp, vp, i32, vp]
+    for name in ("tk_layernorm_forward", "tk_layernorm_backward", "tk_xent_loss", "tk_xent_grad", "tk_xent_status",
+                 "tk_adamw_step", "tk_adamw_set_state", "tk_adamw_get_state"):
+        getattr(lib, name).restype = cint
     for name in ("tk_init", "tk_step", "tk_step_host", "tk_topk", "tk_set_kdown", "tk_last_uplink",
                  "tk_last_aggregate", "tk_last_downlink", "tk_status", "tk_set_profile", "tk_set_force_general"):
         getattr(lib, name).restype = ctypes.c_int
@@ -376,3 +409,253 @@ def tk_topk_noalloc_status() -> int:
 
 def tk_release_scratch() -> None:
     load().tk_release_scratch()
+
+
+# -- training operators --
+
+_TYPES = {torch.float32: TK_F32, torch.bfloat16: TK_BF16}
+
+
+def _type(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise ValueError("expected float32 or bfloat16, got %s" % dtype)
+    return _TYPES[dtype]
+
+
+def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: torch.device, what: str) -> int:
+    """Checks a [rows][dim] matrix whose rows are contiguous; its row stride in values."""
+    if t.shape != (rows, dim) or t.dtype != dtype or t.device != device or (dim > 1 and rows > 0 and t.stride(1) != 1):
+        raise ValueError("%s: expected a [%d][%d] tensor of %s on %s with contiguous rows" % (what, rows, dim, dtype, device))
+    stride = t.stride(0) if rows > 1 else dim
+    if stride < dim:
+        raise ValueError("%s: rows overlap" % what)
+    return stride
+
+
+def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, device: torch.device, what: str) -> int:
+    if t.shape != (n,) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous [%d] tensor of %s on %s" % (what, n, dtype, device))
+    return t.data_ptr()
+
+
+def _enqueue(device: torch.device, stream: Optional[torch.cuda.Stream], call, what: str) -> None:
+    """Runs call(cudaStream_t) with `device` current: on torch's current stream, or on `stream`, ordered
+    after the work that made the inputs and before the work that uses the outputs (both on the current stream)."""
+    if device.type != "cuda":
+        raise ValueError("%s: expected CUDA tensors" % what)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _enqueue(device, stream, call, what)
+    cur = torch.cuda.current_stream(device)
+    if stream is None or stream == cur:
+        return _check(call(cur.cuda_stream), what)
+    stream.wait_stream(cur)
+    try:
+        _check(call(stream.cuda_stream), what)
+    finally:
+        cur.wait_stream(stream)
+
+
+def tk_layernorm_forward(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                         stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Layer norm of every row of x ([rows][dim], rows contiguous): (y, mean, rstd)."""
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows][dim]")
+    (rows, dim), dev = x.shape, x.device
+    xt, pt = _type(x.dtype), _type(gain.dtype)
+    xs = _matrix(x, rows, dim, x.dtype, dev, "x")
+    gp = _vector(gain, dim, gain.dtype, dev, "gain")
+    bp = _vector(bias, dim, gain.dtype, dev, "bias") if bias is not None else None
+    y = torch.empty((rows, dim), dtype=x.dtype, device=dev)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=dev)
+    mean, rstd = stats[0], stats[1]
+    _enqueue(dev, stream, lambda s: load().tk_layernorm_forward(x.data_ptr(), xt, rows, dim, xs, gp, bp, pt, eps, y.data_ptr(), dim,
+                                                                mean.data_ptr(), rstd.data_ptr(), s), "tk_layernorm_forward")
+    return y, mean, rstd
+
+
+def tk_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                          grad_dtype: Optional[torch.dtype] = None, dgain: Optional[torch.Tensor] = None,
+                          dbias: Optional[torch.Tensor] = None, need_dx: bool = True, need_params: bool = True,
+                          stream: Optional[torch.cuda.Stream] = None):
+    """(dx, dgain, dbias) of tk_layernorm_forward; None for what is not needed.  dgain and dbias are made in
+    grad_dtype (default: gain's), or written to the given tensors (for example slices of a gradient row)."""
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows][dim]")
+    (rows, dim), dev = x.shape, x.device
+    if grad_dtype is None:
+        grad_dtype = dgain.dtype if dgain is not None else dbias.dtype if dbias is not None else gain.dtype
+    xt, pt, gt = _type(x.dtype), _type(gain.dtype), _type(grad_dtype)
+    xs, ds = _matrix(x, rows, dim, x.dtype, dev, "x"), _matrix(dy, rows, dim, x.dtype, dev, "dy")
+    gp = _vector(gain, dim, gain.dtype, dev, "gain")
+    mp, rp = _vector(mean, rows, torch.float32, dev, "mean"), _vector(rstd, rows, torch.float32, dev, "rstd")
+    dx = torch.empty((rows, dim), dtype=x.dtype, device=dev) if need_dx else None
+    ws, nbytes = None, 0
+    if need_params:
+        dgain = torch.empty(dim, dtype=grad_dtype, device=dev) if dgain is None else dgain
+        dbias = torch.empty(dim, dtype=grad_dtype, device=dev) if dbias is None else dbias
+        _vector(dgain, dim, grad_dtype, dev, "dgain")
+        _vector(dbias, dim, grad_dtype, dev, "dbias")
+        nbytes = int(load().tk_layernorm_workspace_bytes(rows, dim))
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        dgain = dbias = None
+    _enqueue(dev, stream, lambda s: load().tk_layernorm_backward(
+        dy.data_ptr(), ds, x.data_ptr(), xs, xt, rows, dim, gp, pt, mp, rp, dx.data_ptr() if need_dx else None, dim,
+        dgain.data_ptr() if need_params else None, dbias.data_ptr() if need_params else None, gt,
+        ws.data_ptr() if need_params else None, nbytes, s), "tk_layernorm_backward")
+    return dx, dgain, dbias
+
+
+def _head(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor):
+    if h.dim() != 2 or w.dim() != 2:
+        raise ValueError("expected h [tokens][dim] and w [vocab][dim]")
+    (tokens, dim), vocab, dev = h.shape, w.shape[0], h.device
+    hs, wst = _matrix(h, tokens, dim, h.dtype, dev, "h"), _matrix(w, vocab, dim, h.dtype, dev, "w")
+    tp = _vector(target, tokens, torch.int32, dev, "target")
+    aligned = int(h.data_ptr() % 16 == 0 and w.data_ptr() % 16 == 0 and hs % 8 == 0 and wst % 8 == 0)
+    return tokens, vocab, dim, dev, hs, wst, tp, aligned
+
+
+def tk_xent_workspace_bytes(tokens: int, vocab: int, dim: int, dtype: torch.dtype, grad_dtype: Optional[torch.dtype] = None,
+                            aligned_rows: bool = True) -> int:
+    return int(load().tk_xent_workspace_bytes(tokens, vocab, dim, _type(dtype), -1 if grad_dtype is None else _type(grad_dtype),
+                                              int(aligned_rows)))
+
+
+def _xent_workspace(tokens, vocab, dim, in_type, grad_type, aligned, dev, what):
+    nbytes = int(load().tk_xent_workspace_bytes(tokens, vocab, dim, in_type, grad_type, aligned))
+    if nbytes == 0:
+        raise TkError(-1, what)
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev), nbytes
+
+
+def tk_xent_loss(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
+                 stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, lse) per token of the head h w^T; target int32, negative = takes no part."""
+    tokens, vocab, dim, dev, hs, wst, tp, aligned = _head(h, w, target)
+    it = _type(h.dtype)
+    out = torch.empty((2, tokens), dtype=torch.float32, device=dev)
+    loss, lse = out[0], out[1]
+    ws, nbytes = _xent_workspace(tokens, vocab, dim, it, -1, aligned, dev, "tk_xent_loss")
+    _enqueue(dev, stream, lambda s: load().tk_xent_loss(h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp,
+                                                        loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes, s), "tk_xent_loss")
+    return loss, lse
+
+
+def tk_xent_grad(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                 grad_dtype: Optional[torch.dtype] = None, dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                 need_dh: bool = True, need_dw: bool = True, stream: Optional[torch.cuda.Stream] = None):
+    """(dh, dw) of sum_i dloss_i loss_i, from the lse of tk_xent_loss; None for what is not needed.  They are
+    made in grad_dtype (default: h's), or written to the given tensors (for example a slice of a gradient row)."""
+    tokens, vocab, dim, dev, hs, wst, tp, aligned = _head(h, w, target)
+    if grad_dtype is None:
+        grad_dtype = dw.dtype if dw is not None else dh.dtype if dh is not None else h.dtype
+    it, gt = _type(h.dtype), _type(grad_dtype)
+    lp, dp = _vector(lse, tokens, torch.float32, dev, "lse"), _vector(dloss, tokens, torch.float32, dev, "dloss")
+    dh = (torch.empty((tokens, dim), dtype=grad_dtype, device=dev) if dh is None else dh) if need_dh else None
+    dw = (torch.empty((vocab, dim), dtype=grad_dtype, device=dev) if dw is None else dw) if need_dw else None
+    dhs = _matrix(dh, tokens, dim, grad_dtype, dev, "dh") if need_dh else 0
+    dws = _matrix(dw, vocab, dim, grad_dtype, dev, "dw") if need_dw else 0
+    ws, nbytes = _xent_workspace(tokens, vocab, dim, it, gt, aligned, dev, "tk_xent_grad")
+    _enqueue(dev, stream, lambda s: load().tk_xent_grad(
+        h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp, lp, dp, dh.data_ptr() if need_dh else None, dhs,
+        dw.data_ptr() if need_dw else None, dws, gt, ws.data_ptr(), nbytes, s), "tk_xent_grad")
+    return dh, dw
+
+
+def tk_xent_status() -> int:
+    """Waits for the device; 0, or the negative TK_ERR_* code if a kernel of the cross entropy gave up a wait."""
+    return int(load().tk_xent_status())
+
+
+ADAMW_BLOCK = 256   # consecutive values that share a scale in the 8-bit states
+
+
+class AdamW:
+    """The states of an AdamW optimiser over a list of tensors, and the calls that use them.
+
+    params: contiguous tensors, all fp32 or all bf16, on one device (views of a flat vector are fine).
+    weight_decay: one number, or one per tensor.  copies: per tensor None or a bf16 tensor of the same size
+    that receives the updated parameters."""
+
+    def __init__(self, params, state_bits: int = 32, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay=0.01, copies=None):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no tensors")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits: 8 or 32")
+        self.device, self.dtype = self.params[0].device, self.params[0].dtype
+        self.lr, self.betas, self.eps, self.state_bits, self.steps = lr, betas, eps, state_bits, 0
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
+        if len(decay) != len(self.params) or len(self.copies) != len(self.params):
+            raise ValueError("weight_decay / copies: one per tensor")
+        param_type = _type(self.dtype)
+        for p, c in zip(self.params, self.copies):
+            if p.dtype != self.dtype or p.device != self.device or not p.is_contiguous():
+                raise ValueError("params: expected contiguous tensors of one type on one device")
+            if c is not None and (c.dtype != torch.bfloat16 or c.device != self.device or not c.is_contiguous() or
+                                  c.numel() != p.numel()):
+                raise ValueError("copies: expected contiguous bfloat16 tensors of the parameters' sizes")
+        self.sizes = [p.numel() for p in self.params]
+        blocks = [-(-n // ADAMW_BLOCK) for n in self.sizes]
+        if state_bits == 32:
+            self.m = torch.zeros(sum(self.sizes), dtype=torch.float32, device=self.device)
+            self.scales = None
+            per, step = self.sizes, 4
+        else:
+            self.m = torch.zeros(sum(blocks) * ADAMW_BLOCK, dtype=torch.uint8, device=self.device)
+            self.scales = torch.zeros(sum(blocks) * 2, dtype=torch.float32, device=self.device)
+            per, step = [b * ADAMW_BLOCK for b in blocks], 1
+        self.v = torch.zeros_like(self.m)
+        self._table = (tk_adamw_tensor * len(self.params))()
+        at = block = 0
+        for t, p, c, d, n, b in zip(self._table, self.params, self.copies, decay, per, blocks):
+            t.n, t.param, t.copy16 = p.numel(), p.data_ptr(), c.data_ptr() if c is not None else None
+            t.m, t.v = self.m.data_ptr() + at * step, self.v.data_ptr() + at * step
+            t.scales = self.scales.data_ptr() + 8 * block if state_bits == 8 else None
+            t.weight_decay = d
+            at += n
+            block += b
+        self._options = tk_adamw_options(beta1=betas[0], beta2=betas[1], eps=eps, param_type=param_type, state_bits=state_bits)
+
+    def _pointers(self, tensors, dtype: torch.dtype, what: str):
+        if len(tensors) != len(self.sizes):
+            raise ValueError("%s: expected %d tensors" % (what, len(self.sizes)))
+        for t, n in zip(tensors, self.sizes):
+            if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
+                raise ValueError("%s: expected contiguous tensors of the parameters' sizes, %s, on %s" % (what, dtype, self.device))
+        return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+
+    def tk_adamw_step(self, grads, lr: Optional[float] = None, grad_scale: float = 1.0,
+                      stream: Optional[torch.cuda.Stream] = None) -> None:
+        """One step with these gradients (all fp32 or all bf16); lr overrides the one given at the start."""
+        dtype = grads[0].dtype
+        o = self._options
+        o.grad_type = _type(dtype)
+        ptrs = self._pointers(grads, dtype, "grads")
+        o.lr, o.grad_scale, o.step = self.lr if lr is None else lr, grad_scale, self.steps + 1
+        _enqueue(self.device, stream, lambda s: load().tk_adamw_step(self._table, ptrs, len(ptrs), ctypes.byref(o), s), "tk_adamw_step")
+        self.steps += 1
+
+    def tk_adamw_set_state(self, m, v, step: int, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Takes the states from fp32 values, one tensor per parameter (a checkpoint's), and the number of steps done."""
+        pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
+        if self.state_bits == 8:
+            _enqueue(self.device, stream, lambda s: load().tk_adamw_set_state(self._table, pm, pv, len(pm), s), "tk_adamw_set_state")
+        else:
+            torch._foreach_copy_(list(torch.split(self.m, self.sizes)), [t.reshape(-1) for t in m])
+            torch._foreach_copy_(list(torch.split(self.v, self.sizes)), [t.reshape(-1) for t in v])
+        self.steps = step
+
+    def tk_adamw_get_state(self, m, v, stream: Optional[torch.cuda.Stream] = None) -> int:
+        """Writes the values of the states to fp32 tensors, one per parameter; the number of steps done."""
+        pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
+        if self.state_bits == 8:
+            _enqueue(self.device, stream, lambda s: load().tk_adamw_get_state(self._table, pm, pv, len(pm), s), "tk_adamw_get_state")
+        else:
+            torch._foreach_copy_([t.view(-1) for t in m], list(torch.split(self.m, self.sizes)))
+            torch._foreach_copy_([t.view(-1) for t in v], list(torch.split(self.v, self.sizes)))
+        return self.steps

@@ -9,10 +9,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 # TOPK_LIBRARY selects another build of the library (for example one compiled with different tuning macros)
 LIB = os.environ.get("TOPK_LIBRARY") or os.path.join(_HERE, "libtopk.so")
-SOURCES = ["api.cu"]
-HEADERS = sorted(f for f in os.listdir(CSRC) if f.endswith(".cuh"))   # every header api.cu may include
+SOURCES = ["api.cu", "train.cu"]
+HEADERS = sorted(f for f in os.listdir(CSRC) if f.endswith(".cuh"))   # every header the sources may include
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def _nvcc() -> str:

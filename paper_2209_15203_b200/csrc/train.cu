@@ -1,0 +1,695 @@
+// Host side of the training operators: argument checking, workspace layout, launches.
+// The C ABI is declared and documented in include/topk.h.
+#include "../../include/topk.h"
+
+#include <math.h>
+#include <stddef.h>
+
+#include "adamw.cuh"
+#include "layernorm.cuh"
+#include "xent.cuh"
+
+using namespace tk;
+
+namespace {
+
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+
+bool aligned(const void* p, size_t to) { return p != nullptr && ((uintptr_t)p & (to - 1)) == 0; }
+bool type_ok(int t) { return t == TK_F32 || t == TK_BF16; }
+size_t size_of(int t) { return t == TK_BF16 ? 2 : 4; }
+
+int launch_error() {
+    if (cudaGetLastError() != cudaSuccess) return TK_ERR_CUDA;
+    return TK_OK;
+}
+
+// Raised by a kernel whose bounded wait ran out; zero when the library is loaded.
+__device__ int g_status;
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct Device {
+    bool ready = false;
+    int sms = 0;
+    int* status = nullptr;
+    EncodeFn encode = nullptr;
+};
+Device g_devices[64];
+
+int device(Device** out) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return TK_ERR_CUDA;
+    Device& d = g_devices[dev];
+    if (!d.ready) {
+        void *fn = nullptr, *status = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaGetSymbolAddress(&status, g_status) != cudaSuccess ||
+            cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn) {
+            cudaGetLastError();
+            return TK_ERR_CUDA;
+        }
+        d.status = (int*)status;
+        d.encode = (EncodeFn)fn;
+        d.ready = true;
+    }
+    *out = &d;
+    return TK_OK;
+}
+
+}  // namespace
+
+// =============================================== layer norm ===============================================
+
+namespace {
+
+constexpr int kNormMaxParts = 296;   // rows of partial sums: CTAs of the backward kernel, two per SM
+constexpr int kNormWideParts = 32;
+constexpr int kNormMaxDim = 1 << 24;
+
+struct NormShape {
+    int vec, nv, group;   // values per load, loads per thread, threads per row; group 0: the wide kernels
+};
+
+// The smallest group whose threads hold a row in at most 4 loads of 16 bytes each (or 8 single values).
+NormShape norm_shape(int dim, int type, bool wide_loads) {
+    const int vec = wide_loads ? (type == TK_BF16 ? 8 : 4) : 1;
+    const int vectors = (dim + vec - 1) / vec;
+    const int most = wide_loads ? 4 : 8;
+    for (int group : {32, 128, 512, 1024})
+        if (vectors <= group * most) {
+            int nv = 1;
+            while (group * nv < vectors) nv *= 2;
+            return {vec, nv, group};
+        }
+    return {vec, 0, 0};
+}
+
+template <typename T, int VEC, int NV, int G>
+int launch_norm(const NormArgs& a, bool backward, int grid, cudaStream_t s) {
+    const int threads = G > kNormThreads ? G : kNormThreads;
+    if (backward) {
+        const size_t smem = threads / G > 1 ? (size_t)2 * a.dim * sizeof(float) : 0;
+        norm_backward_kernel<T, VEC, NV, G><<<grid, threads, smem, s>>>(a);
+    } else {
+        norm_forward_kernel<T, VEC, NV, G><<<grid, threads, 0, s>>>(a);
+    }
+    return launch_error();
+}
+template <typename T, int VEC, int G>
+int launch_norm(int nv, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
+    switch (nv) {
+        case 1: return launch_norm<T, VEC, 1, G>(a, backward, grid, s);
+        case 2: return launch_norm<T, VEC, 2, G>(a, backward, grid, s);
+        case 4: return launch_norm<T, VEC, 4, G>(a, backward, grid, s);
+        default:
+            if (VEC == 1) return launch_norm<T, VEC, VEC == 1 ? 8 : 4, G>(a, backward, grid, s);
+            return TK_ERR_INTERNAL;
+    }
+}
+template <typename T, int VEC>
+int launch_norm(const NormShape& f, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
+    switch (f.group) {
+        case 32: return launch_norm<T, VEC, 32>(f.nv, a, backward, grid, s);
+        case 128: return launch_norm<T, VEC, 128>(f.nv, a, backward, grid, s);
+        case 512: return launch_norm<T, VEC, 512>(f.nv, a, backward, grid, s);
+        default: return launch_norm<T, VEC, 1024>(f.nv, a, backward, grid, s);
+    }
+}
+int launch_norm(const NormShape& f, int type, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
+    if (type == TK_BF16)
+        return f.vec > 1 ? launch_norm<bf16, 8>(f, a, backward, grid, s) : launch_norm<bf16, 1>(f, a, backward, grid, s);
+    return f.vec > 1 ? launch_norm<float, 4>(f, a, backward, grid, s) : launch_norm<float, 1>(f, a, backward, grid, s);
+}
+
+bool norm_args_ok(int64_t rows, int64_t dim, int x_type, int param_type) {
+    return rows >= 0 && rows < ((int64_t)1 << 40) && dim >= 1 && dim <= kNormMaxDim && type_ok(x_type) && type_ok(param_type);
+}
+bool rows_ok(const void* p, int type, int64_t stride, int64_t dim) {
+    return aligned(p, size_of(type)) && stride >= dim && stride < ((int64_t)1 << 40);
+}
+// Whether every row of `dim` values starts on a 16-byte boundary (and ends on one)
+bool rows_wide(const void* p, int type, int64_t stride, int64_t dim) {
+    const size_t e = size_of(type);
+    return p == nullptr || (aligned(p, 16) && stride * e % 16 == 0 && dim * e % 16 == 0);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tk_layernorm_forward(const void* x, int x_type, int64_t rows, int64_t dim, int64_t x_stride, const void* gain, const void* bias,
+                         int param_type, float eps, void* y, int64_t y_stride, float* mean, float* rstd, void* cuda_stream) {
+    if (!norm_args_ok(rows, dim, x_type, param_type) || !(eps >= 0.0f) || isinf(eps)) return TK_ERR_INVALID;
+    if ((mean == nullptr) != (rstd == nullptr)) return TK_ERR_INVALID;
+    if (!aligned(gain, size_of(param_type)) || (bias && !aligned(bias, size_of(param_type)))) return TK_ERR_INVALID;
+    if (rows == 0) return TK_OK;
+    if (!rows_ok(x, x_type, x_stride, dim) || !rows_ok(y, x_type, y_stride, dim)) return TK_ERR_INVALID;
+    if (mean && (!aligned(mean, 4) || !aligned(rstd, 4))) return TK_ERR_INVALID;
+    Device* d;
+    int rc = device(&d);
+    if (rc != TK_OK) return rc;
+    const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(y, x_type, y_stride, dim) && aligned(gain, 16) &&
+                      (!bias || aligned(bias, 16));
+    const NormShape f = norm_shape((int)dim, x_type, wide);
+    NormArgs a = {};
+    a.x = x, a.out = y, a.gain = gain, a.bias = bias, a.mean = mean, a.rstd = rstd;
+    a.rows = rows, a.x_stride = x_stride, a.out_stride = y_stride;
+    a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16, a.eps = eps;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (!f.group) {
+        const int grid = (int)(rows < 4 * d->sms ? rows : 4 * d->sms);
+        if (x_type == TK_BF16)
+            norm_wide_kernel<bf16><<<grid, 1024, 0, s>>>(a, 0);
+        else
+            norm_wide_kernel<float><<<grid, 1024, 0, s>>>(a, 0);
+        return launch_error();
+    }
+    const int per_cta = f.group > kNormThreads ? 1 : kNormThreads / f.group;
+    const int64_t ctas = (rows + per_cta - 1) / per_cta, most = (int64_t)d->sms * 64;
+    return launch_norm(f, x_type, a, false, (int)(ctas < most ? ctas : most), s);
+}
+
+size_t tk_layernorm_workspace_bytes(int64_t rows, int64_t dim) {
+    if (rows < 0 || dim < 1 || dim > kNormMaxDim) return 0;
+    return align_up((size_t)kNormMaxParts * 2 * (size_t)dim * sizeof(float));
+}
+
+int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int x_type, int64_t rows, int64_t dim,
+                          const void* gain, int param_type, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                          void* dgain, void* dbias, int grad_type, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!norm_args_ok(rows, dim, x_type, param_type) || !type_ok(grad_type)) return TK_ERR_INVALID;
+    if (!aligned(gain, size_of(param_type))) return TK_ERR_INVALID;
+    if ((dgain && !aligned(dgain, size_of(grad_type))) || (dbias && !aligned(dbias, size_of(grad_type)))) return TK_ERR_INVALID;
+    if (!dx && !dgain && !dbias) return TK_ERR_INVALID;
+    if (rows > 0) {
+        if (!rows_ok(x, x_type, x_stride, dim) || !rows_ok(dy, x_type, dy_stride, dim)) return TK_ERR_INVALID;
+        if (dx && !rows_ok(dx, x_type, dx_stride, dim)) return TK_ERR_INVALID;
+        if (!aligned(mean, 4) || !aligned(rstd, 4)) return TK_ERR_INVALID;
+    }
+    const bool params = dgain || dbias;
+    if (params && (!aligned(workspace, 16) || workspace_bytes < tk_layernorm_workspace_bytes(rows, dim))) return TK_ERR_ALLOC;
+    Device* d;
+    int rc = device(&d);
+    if (rc != TK_OK) return rc;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    int parts = 0;
+    if (rows > 0) {
+        const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(dy, x_type, dy_stride, dim) &&
+                          rows_wide(dx, x_type, dx_stride, dim) && aligned(gain, 16);
+        const NormShape f = norm_shape((int)dim, x_type, wide);
+        NormArgs a = {};
+        a.x = x, a.dy = dy, a.out = dx, a.gain = gain, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
+        a.partial = params ? (float*)workspace : nullptr;
+        a.rows = rows, a.x_stride = x_stride, a.dy_stride = dy_stride, a.out_stride = dx_stride;
+        a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16;
+        if (!f.group) {
+            const int grid = (int)(rows < 4 * d->sms ? rows : 4 * d->sms);
+            parts = (int)(rows < kNormWideParts ? rows : kNormWideParts);
+            const dim3 columns((unsigned)((dim + kNormThreads - 1) / kNormThreads), (unsigned)parts);
+            if (x_type == TK_BF16) {
+                if (dx) norm_wide_kernel<bf16><<<grid, 1024, 0, s>>>(a, 1);
+                if (params) norm_columns_kernel<bf16><<<columns, kNormThreads, 0, s>>>(a);
+            } else {
+                if (dx) norm_wide_kernel<float><<<grid, 1024, 0, s>>>(a, 1);
+                if (params) norm_columns_kernel<float><<<columns, kNormThreads, 0, s>>>(a);
+            }
+            rc = launch_error();
+        } else {
+            const int per_cta = f.group > kNormThreads ? 1 : kNormThreads / f.group;
+            const int64_t ctas = (rows + per_cta - 1) / per_cta;
+            const int64_t most = 2 * d->sms < kNormMaxParts ? 2 * d->sms : kNormMaxParts;
+            parts = (int)(ctas < most ? ctas : most);
+            rc = launch_norm(f, x_type, a, true, parts, s);
+        }
+        if (rc != TK_OK) return rc;
+    }
+    if (params) {
+        const unsigned grid = (unsigned)((2 * dim + kNormFinishCols - 1) / kNormFinishCols);
+        norm_finish_kernel<<<grid, kNormFinishCols * kNormFinishSlices, 0, s>>>((const float*)workspace, parts, (int)dim, dgain, dbias,
+                                                                                grad_type == TK_BF16);
+        rc = launch_error();
+    }
+    return rc;
+}
+
+}  // extern "C"
+
+// =============================================== cross entropy ============================================
+
+namespace {
+
+// D of one piece of the vocabulary takes at most this much of the workspace, if a piece of 256 entries fits.
+constexpr size_t kXentPieceBytes = (size_t)256 << 20;
+
+struct XentLayout {
+    int in_parts, d_parts;       // bf16 matrices an input / D is held as
+    bool pack;                   // inputs are copied (fp32, or rows that TMA cannot address)
+    int ld;                      // row of a packed input
+    int64_t piece;               // vocabulary entries per piece, a multiple of 256
+    int tiles_v;
+    size_t off_h, off_w, off_partial, off_picked, off_d, off_acc, bytes;
+};
+
+bool xent_sizes_ok(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type) {
+    if (tokens < 0 || tokens > (1 << 24) || vocab < 1 || vocab > (1 << 26) || dim < 1 || dim > (1 << 20)) return false;
+    if (!type_ok(in_type)) return false;
+    return grad_type < 0 || type_ok(grad_type) && !(in_type == TK_F32 && grad_type == TK_BF16);
+}
+
+XentLayout xent_layout(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type, bool aligned_rows) {
+    XentLayout L = {};
+    L.in_parts = in_type == TK_F32 ? 3 : 1;
+    L.d_parts = grad_type == TK_F32 ? 3 : 1;
+    L.pack = in_type == TK_F32 || !aligned_rows;
+    L.ld = (int)((dim + 7) / 8 * 8);
+    L.tiles_v = (int)((vocab + kTileN - 1) / kTileN);
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        size_t o = at;
+        at += align_up(n);
+        return o;
+    };
+    if (L.pack) {
+        L.off_h = take((size_t)L.in_parts * tokens * L.ld * 2);
+        L.off_w = take((size_t)L.in_parts * vocab * L.ld * 2);
+    }
+    const size_t inputs = at;
+    // the loss's own scratch and the gradient's are never alive together
+    L.off_partial = take((size_t)L.tiles_v * tokens * sizeof(float2));
+    L.off_picked = take((size_t)tokens * sizeof(float));
+    const size_t loss_end = at;
+    at = inputs;
+    if (grad_type >= 0) {
+        const size_t row = (size_t)L.d_parts * 2 * (tokens > 0 ? tokens : 1);
+        int64_t piece = (int64_t)(kXentPieceBytes / row) / kTileN * kTileN;
+        const int64_t all = (vocab + kTileN - 1) / kTileN * kTileN;
+        if (piece < kTileN) piece = kTileN;
+        if (piece > all) piece = all;
+        const int64_t pieces = (all + piece - 1) / piece;   // of equal size, up to a tile
+        L.piece = ((all + pieces - 1) / pieces + kTileN - 1) / kTileN * kTileN;
+        L.off_d = take(row * L.piece);
+        L.off_acc = take((size_t)tokens * dim * sizeof(float));
+    }
+    if (at < loss_end) at = loss_end;
+    L.bytes = at + 256;
+    return L;
+}
+
+// A matrix of `rows` rows of `cols` bf16 values, `parts` of them one after the other, in boxes of 64 x box_rows
+int make_map(Device* d, CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t stride, int parts, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    CUresult rc = d->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, step,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? TK_OK : TK_ERR_CUDA;
+}
+
+// A product's part pairs by rising size: all pairs when one side is a single part, else those of order <= 2
+void set_segments(XentProblem& p, int parts_a, int parts_b) {
+    p.nseg = 0;
+    for (int order = 2; order >= 0; --order)
+        for (int a = 0; a <= order; ++a)
+            if (a < parts_a && order - a < parts_b) {
+                p.sa[p.nseg] = (unsigned char)a;
+                p.sb[p.nseg++] = (unsigned char)(order - a);
+            }
+}
+
+template <int MODE, int CG, int PARTS>
+int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
+    auto kernel = xent_kernel<MODE, CG, PARTS>;
+    constexpr int smem = XentShape<CG>::kSmem;
+    static bool ready[64];
+    static int pairs[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return TK_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kXentThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (!ready[dev]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+            cudaGetLastError();
+            return TK_ERR_CUDA;
+        }
+        cfg.gridDim = dim3((unsigned)(d->sms / CG * CG));
+        if (cudaOccupancyMaxActiveClusters(&pairs[dev], kernel, &cfg) != cudaSuccess || pairs[dev] < 1) {
+            cudaGetLastError();
+            return TK_ERR_CUDA;
+        }
+        ready[dev] = true;
+    }
+    const u32 workers = a.tiles < (u32)pairs[dev] ? a.tiles : (u32)pairs[dev];
+    cfg.gridDim = dim3(workers * CG);
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
+        cudaGetLastError();
+        return TK_ERR_CUDA;
+    }
+    return TK_OK;
+}
+
+template <typename T, int PARTS>
+int launch_pack(Device* d, const void* x, int64_t stride, int64_t rows, int64_t dim, int ld, void* out, cudaStream_t s) {
+    const int64_t ctas = (rows * ld + 255) / 256, most = (int64_t)d->sms * 32;
+    if (ctas == 0) return TK_OK;
+    xent_pack_kernel<T, PARTS><<<(unsigned)(ctas < most ? ctas : most), 256, 0, s>>>((const T*)x, stride, rows, (int)dim, ld, (bf16*)out);
+    return launch_error();
+}
+
+struct XentInputs {
+    const void *h, *w;            // as the matrix kernel reads them: bf16, parts one after the other
+    int64_t h_stride, w_stride;
+};
+
+// Copies the inputs to the workspace if the kernel cannot read them where they are.
+int xent_inputs(Device* d, const XentLayout& L, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type,
+                int64_t tokens, int64_t vocab, int64_t dim, char* ws, XentInputs* out, cudaStream_t s) {
+    if (!L.pack) {
+        *out = {h, w, h_stride, w_stride};
+        return TK_OK;
+    }
+    *out = {ws + L.off_h, ws + L.off_w, L.ld, L.ld};
+    int rc;
+    if (in_type == TK_F32) {
+        rc = launch_pack<float, 3>(d, h, h_stride, tokens, dim, L.ld, ws + L.off_h, s);
+        if (rc == TK_OK) rc = launch_pack<float, 3>(d, w, w_stride, vocab, dim, L.ld, ws + L.off_w, s);
+    } else {
+        rc = launch_pack<bf16, 1>(d, h, h_stride, tokens, dim, L.ld, ws + L.off_h, s);
+        if (rc == TK_OK) rc = launch_pack<bf16, 1>(d, w, w_stride, vocab, dim, L.ld, ws + L.off_w, s);
+    }
+    return rc;
+}
+
+bool xent_rows_aligned(const void* p, int64_t stride) { return aligned(p, 16) && stride % 8 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+size_t tk_xent_workspace_bytes(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type, int aligned_rows) {
+    if (!xent_sizes_ok(tokens, vocab, dim, in_type, grad_type)) return 0;
+    return xent_layout(tokens, vocab, dim, in_type, grad_type, aligned_rows != 0).bytes;
+}
+
+int tk_xent_loss(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type, int64_t tokens, int64_t vocab,
+                 int64_t dim, const int32_t* target, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                 void* cuda_stream) {
+    if (!xent_sizes_ok(tokens, vocab, dim, in_type, -1)) return TK_ERR_INVALID;
+    if (!rows_ok(w, in_type, w_stride, dim)) return TK_ERR_INVALID;
+    if (tokens == 0) return TK_OK;
+    if (!rows_ok(h, in_type, h_stride, dim) || !aligned(target, 4) || !aligned(loss, 4) || !aligned(lse, 4)) return TK_ERR_INVALID;
+    const XentLayout L = xent_layout(tokens, vocab, dim, in_type, -1, xent_rows_aligned(h, h_stride) && xent_rows_aligned(w, w_stride));
+    if (!aligned(workspace, 256) || workspace_bytes < L.bytes) return TK_ERR_ALLOC;
+    Device* d;
+    int rc = device(&d);
+    if (rc != TK_OK) return rc;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    char* ws = (char*)workspace;
+    XentInputs in;
+    rc = xent_inputs(d, L, h, h_stride, w, w_stride, in_type, tokens, vocab, dim, ws, &in, s);
+    if (rc != TK_OK) return rc;
+    constexpr int CG = 1;
+    XentArgs a = {};
+    XentProblem& p = a.p[0];
+    rc = make_map(d, &p.a, in.h, dim, tokens, in.h_stride, L.in_parts, kTileM);
+    if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / CG);
+    if (rc != TK_OK) return rc;
+    p.tiles_m = (int)((tokens + kTileM * CG - 1) / (kTileM * CG));
+    p.tiles_n = L.tiles_v;
+    p.kblocks = (int)((dim + kTileK - 1) / kTileK);
+    p.cols = (int)vocab;
+    set_segments(p, L.in_parts, L.in_parts);
+    if ((int64_t)p.tiles_m * p.tiles_n >= ((int64_t)1 << 31)) return TK_ERR_INVALID;
+    a.tiles0 = a.tiles = (u32)(p.tiles_m * p.tiles_n);
+    a.tokens = (int)tokens, a.vocab = (int)vocab, a.target = target;
+    a.partial = (float2*)(ws + L.off_partial);
+    a.picked = (float*)(ws + L.off_picked);
+    a.status = d->status;
+    rc = launch_xent<kXentLoss, CG, 1>(d, a, s);
+    if (rc != TK_OK) return rc;
+    // few rows: many lanes per row; from 32 rows a warp on, the loads of a warp are whole lines with one lane each
+    const int lanes = tokens >= 8192 ? 1 : (tokens >= 1024 ? 4 : 32);
+    const int64_t warps = (tokens + 32 / lanes - 1) / (32 / lanes);
+    xent_join_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a.partial, a.picked, target, (int)tokens, (int)vocab, L.tiles_v, lanes,
+                                                                 loss, lse);
+    return launch_error();
+}
+
+int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type, int64_t tokens, int64_t vocab,
+                 int64_t dim, const int32_t* target, const float* lse, const float* dloss, void* dh, int64_t dh_stride, void* dw,
+                 int64_t dw_stride, int grad_type, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (grad_type < 0 || !xent_sizes_ok(tokens, vocab, dim, in_type, grad_type)) return TK_ERR_INVALID;
+    if (!dh && !dw) return TK_ERR_INVALID;
+    if (!rows_ok(w, in_type, w_stride, dim)) return TK_ERR_INVALID;
+    if (dw && !rows_ok(dw, grad_type, dw_stride, dim)) return TK_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    const size_t e = size_of(grad_type);
+    if (tokens == 0) {
+        if (dw && cudaMemset2DAsync(dw, dw_stride * e, 0, dim * e, vocab, s) != cudaSuccess) {
+            cudaGetLastError();
+            return TK_ERR_CUDA;
+        }
+        return TK_OK;
+    }
+    if (!rows_ok(h, in_type, h_stride, dim) || !aligned(target, 4) || !aligned(lse, 4) || !aligned(dloss, 4)) return TK_ERR_INVALID;
+    if (dh && !rows_ok(dh, grad_type, dh_stride, dim)) return TK_ERR_INVALID;
+    const XentLayout L =
+        xent_layout(tokens, vocab, dim, in_type, grad_type, xent_rows_aligned(h, h_stride) && xent_rows_aligned(w, w_stride));
+    if (!aligned(workspace, 256) || workspace_bytes < L.bytes) return TK_ERR_ALLOC;
+    Device* d;
+    int rc = device(&d);
+    if (rc != TK_OK) return rc;
+    char* ws = (char*)workspace;
+    XentInputs in;
+    rc = xent_inputs(d, L, h, h_stride, w, w_stride, in_type, tokens, vocab, dim, ws, &in, s);
+    if (rc != TK_OK) return rc;
+    constexpr int CG = 1;
+    const int grad_rows = kTileM * CG;
+    XentArgs soft = {}, grad = {};
+    {
+        XentProblem& p = soft.p[0];
+        rc = make_map(d, &p.a, in.h, dim, tokens, in.h_stride, L.in_parts, kTileM);
+        if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / CG);
+        if (rc == TK_OK) rc = make_map(d, &soft.store, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, 32);
+        if (rc != TK_OK) return rc;
+        p.tiles_m = (int)((tokens + grad_rows - 1) / grad_rows);
+        p.kblocks = (int)((dim + kTileK - 1) / kTileK);
+        p.cols = (int)vocab;
+        set_segments(p, L.in_parts, L.in_parts);
+        soft.tokens = (int)tokens, soft.vocab = (int)vocab, soft.target = target, soft.lse = lse, soft.dloss = dloss;
+        soft.status = grad.status = d->status;
+        grad.tokens = (int)tokens, grad.vocab = (int)vocab;
+    }
+    XentProblem pw = {}, ph = {};
+    if (dw) {   // dw[v][:] = sum over tokens of D[t][v] h[t][:]
+        rc = make_map(d, &pw.a, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, 64);
+        if (rc == TK_OK) rc = make_map(d, &pw.b, in.h, dim, tokens, in.h_stride, L.in_parts, 64);
+        if (rc != TK_OK) return rc;
+        pw.a_mn = pw.b_mn = 1;
+        pw.tiles_n = (int)((dim + kTileN - 1) / kTileN);
+        pw.kblocks = (int)((tokens + kTileK - 1) / kTileK);
+        pw.cols = (int)dim;
+        set_segments(pw, L.d_parts, L.in_parts);
+        pw.ld = dw_stride, pw.out_bf16 = grad_type == TK_BF16;
+    }
+    if (dh) {   // dh[t][:] = sum over the vocabulary of D[t][v] w[v][:]
+        rc = make_map(d, &ph.a, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, kTileM);
+        if (rc == TK_OK) rc = make_map(d, &ph.b, in.w, dim, vocab, in.w_stride, L.in_parts, 64);
+        if (rc != TK_OK) return rc;
+        ph.b_mn = 1;
+        ph.tiles_m = soft.p[0].tiles_m;
+        ph.tiles_n = (int)((dim + kTileN - 1) / kTileN);
+        ph.cols = (int)dim;
+        set_segments(ph, L.d_parts, L.in_parts);
+        ph.acc = (float*)(ws + L.off_acc);
+        ph.ld = dh_stride, ph.rows = tokens, ph.out_bf16 = grad_type == TK_BF16;
+    }
+    for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
+        const int64_t here = vocab - v0 < L.piece ? vocab - v0 : L.piece;
+        const bool first = v0 == 0, last = v0 + here == vocab;
+        XentProblem& p = soft.p[0];
+        p.tiles_n = (int)((here + kTileN - 1) / kTileN);
+        p.b_off = (int)v0;
+        soft.v0 = (int)v0;
+        soft.tiles0 = soft.tiles = (u32)(p.tiles_m * p.tiles_n);
+        rc = L.d_parts == 1 ? launch_xent<kXentSoft, CG, 1>(d, soft, s) : launch_xent<kXentSoft, CG, 3>(d, soft, s);
+        if (rc != TK_OK) return rc;
+        int n = 0;
+        grad.tiles0 = grad.tiles = 0;
+        u32 tiles[2] = {0, 0};
+        if (dh) {
+            ph.kblocks = (int)((here + kTileK - 1) / kTileK);
+            ph.b_koff = (int)v0;
+            ph.acc_read = !first, ph.acc_write = !last;
+            ph.out = last ? dh : nullptr;
+            tiles[n] = (u32)(ph.tiles_m * ph.tiles_n);
+            grad.p[n++] = ph;
+        }
+        if (dw) {
+            pw.tiles_m = (int)((here + grad_rows - 1) / grad_rows);
+            pw.rows = here;
+            pw.out = (char*)dw + v0 * dw_stride * e;
+            tiles[n] = (u32)(pw.tiles_m * pw.tiles_n);
+            grad.p[n++] = pw;
+        }
+        grad.tiles0 = tiles[0], grad.tiles = tiles[0] + tiles[1];
+        rc = launch_xent<kXentGrad, CG, 1>(d, grad, s);
+        if (rc != TK_OK) return rc;
+    }
+    return TK_OK;
+}
+
+int tk_xent_status(void) {
+    Device* d;
+    int rc = device(&d);
+    if (rc != TK_OK) return rc;
+    int status = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&status, d->status, sizeof status, cudaMemcpyDeviceToHost) != cudaSuccess ||
+        (status != 0 && cudaMemset(d->status, 0, sizeof status) != cudaSuccess)) {
+        cudaGetLastError();
+        return TK_ERR_CUDA;
+    }
+    return status ? TK_ERR_INTERNAL : TK_OK;
+}
+
+}  // extern "C"
+
+// =============================================== AdamW ====================================================
+
+namespace {
+
+bool adam_tensor_ok(const tk_adamw_tensor& t, int param_type, int bits) {
+    if (t.n < 0 || t.n >= ((int64_t)1 << 40)) return false;
+    if (t.n == 0) return true;
+    if (!aligned(t.m, bits == 8 ? 8 : 4) || !aligned(t.v, bits == 8 ? 8 : 4)) return false;
+    if (bits == 8 && !aligned(t.scales, 8)) return false;
+    return param_type < 0 || (aligned(t.param, size_of(param_type)) && (!t.copy16 || aligned(t.copy16, 2)) && isfinite(t.weight_decay));
+}
+
+template <int CAP, typename Fill, typename Run>
+int adam_launches(const tk_adamw_tensor* tensors, int32_t count, AdamGroup<CAP>& g, Fill fill, Run run) {
+    int64_t chunks = 0;
+    g.count = 0;
+    for (int32_t i = 0; i <= count; ++i) {
+        int64_t need = 0;
+        if (i < count) {
+            if (tensors[i].n == 0) continue;
+            need = (tensors[i].n + (int64_t)kAdamBlock * kAdamChunk - 1) / ((int64_t)kAdamBlock * kAdamChunk);
+        }
+        if (g.count > 0 && (i == count || g.count == CAP || chunks + need >= ((int64_t)1 << 31))) {
+            int rc = run(g, (unsigned)chunks);
+            if (rc != TK_OK) return rc;
+            g.count = 0;
+            chunks = 0;
+        }
+        if (i == count) break;
+        AdamEntry& e = g.e[g.count++];
+        e.n = tensors[i].n;
+        e.m = (char*)tensors[i].m;
+        e.v = (char*)tensors[i].v;
+        e.scales = (float2*)tensors[i].scales;
+        e.first = (u32)chunks;
+        fill(e, i);
+        chunks += need;
+    }
+    return TK_OK;
+}
+
+template <int CAP>
+int adam_step(const tk_adamw_tensor* tensors, const void* const* grads, int32_t count, const tk_adamw_options* o, cudaStream_t s) {
+    AdamGroup<CAP> g;
+    g.h.b1 = (float)o->beta1, g.h.c1 = (float)(1.0 - o->beta1);
+    g.h.b2 = (float)o->beta2, g.h.c2 = (float)(1.0 - o->beta2);
+    g.h.eps = (float)o->eps;
+    g.h.lr1 = (float)(o->lr / (1.0 - pow(o->beta1, (double)o->step)));
+    g.h.rbc2 = (float)(1.0 / sqrt(1.0 - pow(o->beta2, (double)o->step)));
+    g.h.gscale = (float)o->grad_scale;
+    g.scaled = o->grad_scale != 1.0;
+    auto fill = [&](AdamEntry& e, int32_t i) {
+        e.p = (char*)tensors[i].param;
+        e.g = (const char*)grads[i];
+        e.copy16 = (bf16*)tensors[i].copy16;
+        e.decay = (float)(o->lr * tensors[i].weight_decay);
+    };
+    auto run = [&](const AdamGroup<CAP>& a, unsigned grid) {
+        const int which = (o->param_type == TK_BF16) * 4 + (o->grad_type == TK_BF16) * 2 + (o->state_bits == 8);
+        switch (which) {
+            case 0: adamw_kernel<float, float, 32, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 1: adamw_kernel<float, float, 8, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 2: adamw_kernel<float, bf16, 32, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 3: adamw_kernel<float, bf16, 8, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 4: adamw_kernel<bf16, float, 32, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 5: adamw_kernel<bf16, float, 8, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            case 6: adamw_kernel<bf16, bf16, 32, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+            default: adamw_kernel<bf16, bf16, 8, CAP><<<grid, kAdamThreads, 0, s>>>(a); break;
+        }
+        return launch_error();
+    };
+    return adam_launches<CAP>(tensors, count, g, fill, run);
+}
+
+template <bool LOAD, int CAP>
+int adam_state(const tk_adamw_tensor* tensors, float* const* m, float* const* v, int32_t count, cudaStream_t s) {
+    AdamGroup<CAP> g = {};
+    auto fill = [&](AdamEntry& e, int32_t i) {
+        e.p = (char*)m[i];
+        e.g = (const char*)v[i];
+    };
+    auto run = [&](const AdamGroup<CAP>& a, unsigned grid) {
+        adamw_state_kernel<LOAD, CAP><<<grid, kAdamThreads, 0, s>>>(a);
+        return launch_error();
+    };
+    return adam_launches<CAP>(tensors, count, g, fill, run);
+}
+
+int adam_state_checked(const tk_adamw_tensor* tensors, float* const* m, float* const* v, int32_t count, bool load, void* cuda_stream) {
+    if (count < 0 || (count > 0 && (!tensors || !m || !v))) return TK_ERR_INVALID;
+    for (int32_t i = 0; i < count; ++i)
+        if (!adam_tensor_ok(tensors[i], -1, 8) || (tensors[i].n > 0 && (!aligned(m[i], 4) || !aligned(v[i], 4)))) return TK_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (count <= kAdamSmallCap)
+        return load ? adam_state<true, kAdamSmallCap>(tensors, m, v, count, s) : adam_state<false, kAdamSmallCap>(tensors, m, v, count, s);
+    return load ? adam_state<true, kAdamLargeCap>(tensors, m, v, count, s) : adam_state<false, kAdamLargeCap>(tensors, m, v, count, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tk_adamw_step(const tk_adamw_tensor* tensors, const void* const* grads, int32_t count, const tk_adamw_options* o,
+                  void* cuda_stream) {
+    if (!o || count < 0 || (count > 0 && (!tensors || !grads))) return TK_ERR_INVALID;
+    if (!type_ok(o->param_type) || !type_ok(o->grad_type) || (o->state_bits != 8 && o->state_bits != 32)) return TK_ERR_INVALID;
+    if (!isfinite(o->lr) || !(o->beta1 >= 0.0 && o->beta1 < 1.0) || !(o->beta2 >= 0.0 && o->beta2 < 1.0) || !(o->eps >= 0.0) ||
+        !isfinite(o->eps) || !isfinite(o->grad_scale) || o->step < 1)
+        return TK_ERR_INVALID;
+    for (int32_t i = 0; i < count; ++i)
+        if (!adam_tensor_ok(tensors[i], o->param_type, o->state_bits) || (tensors[i].n > 0 && !aligned(grads[i], size_of(o->grad_type))))
+            return TK_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    return count <= kAdamSmallCap ? adam_step<kAdamSmallCap>(tensors, grads, count, o, s)
+                                  : adam_step<kAdamLargeCap>(tensors, grads, count, o, s);
+}
+
+int tk_adamw_set_state(const tk_adamw_tensor* tensors, const float* const* m, const float* const* v, int32_t count, void* cuda_stream) {
+    return adam_state_checked(tensors, (float* const*)m, (float* const*)v, count, true, cuda_stream);
+}
+int tk_adamw_get_state(const tk_adamw_tensor* tensors, float* const* m, float* const* v, int32_t count, void* cuda_stream) {
+    return adam_state_checked(tensors, m, v, count, false, cuda_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,39 @@
+// Shared device-side pieces of the training operators (layer norm, cross entropy, AdamW):
+// element types, conversions, warp and group reductions.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace tk {
+
+typedef unsigned int u32;
+typedef unsigned long long u64;
+typedef __nv_bfloat16 bf16;
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// One value of a tensor whose type (fp32 or bf16) is known at run time only; used for vectors of
+// `dim` values that stay in cache, where a uniform branch costs nothing that can be measured.
+__device__ __forceinline__ float load_any(const void* p, int64_t i, bool is_bf16) {
+    return is_bf16 ? to_float(((const bf16*)p)[i]) : ((const float*)p)[i];
+}
+__device__ __forceinline__ void store_any(void* p, int64_t i, float v, bool is_bf16) {
+    if (is_bf16)
+        ((bf16*)p)[i] = from_float<bf16>(v);
+    else
+        ((float*)p)[i] = v;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+}  // namespace tk
