@@ -17,15 +17,17 @@ __device__ __forceinline__ void mbar_init(u32 bar, u32 count) {
 __device__ __forceinline__ void mbar_expect(u32 bar, u32 bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// `bar` is a shared::cluster address (mapped_addr), of this CTA or of its pair
+// `bar` is a shared::cluster address (mapped_addr), of this CTA or of its pair.  Nothing but the order of tensor memory
+// accesses hangs on it, which tcgen05.fence keeps; a release at cluster scope would wait for every store
+// the thread has in flight.
 __device__ __forceinline__ void mbar_arrive_cluster(u32 bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(u32 bar, u32 parity) {
     u32 done;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(done)
         : "r"(bar), "r"(parity)
@@ -77,6 +79,21 @@ __device__ __forceinline__ void tma_load(u32 dst, const CUtensorMap* map, u32 ba
             "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
             : "memory");
 }
+template <int CG>
+__device__ __forceinline__ void tma_load4(u32 dst, const CUtensorMap* map, u32 bar, int x, int y, int z, int u) {
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], "
+            "[%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(u)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, "
+            "%6}], [%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(u)
+            : "memory");
+}
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, u32 src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src),
                  "r"(x), "r"(y), "r"(z)
@@ -120,6 +137,16 @@ __device__ __forceinline__ void tmem_load32(u32 addr, float (&v)[32]) {
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
           "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_load16(u32 addr, float (&v)[16]) {
+    u32* r = (u32*)v;
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
 }
 

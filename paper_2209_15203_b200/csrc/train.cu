@@ -252,8 +252,47 @@ struct XentLayout {
     int ld;                      // row of a packed input
     int64_t piece;               // vocabulary entries per piece, a multiple of 256
     int tiles_v;
-    size_t off_h, off_w, off_partial, off_picked, off_d, off_acc, bytes;
+    int cg;                      // CTAs per tile: 2 (256 rows) unless one tile of 128 rows holds all tokens
+    int dh_per, dw_per;          // rounds of a tile per item of the two gradient products
+    size_t off_h, off_w, off_partial, off_picked, off_d, off_acc, off_dh_part, off_dw_part, bytes;
 };
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int xent_pairs(int parts_a, int parts_b) { return parts_a == 1 || parts_b == 1 ? parts_a * parts_b : 6; }
+
+// Cutting the tiles of the two gradient products into items.  The workers take items in turn (dh's, then dw's), so the
+// launch lasts as long as the worker with the most rounds; whole tiles leave up to half of them idle at the end (8192
+// tokens, 768 wide: 96 + 150 tiles for 74 pairs).  Cut tiles are summed through memory, at a cost of about
+// kItemCost rounds each.  The best of all splits up to kMaxSplits each is taken.
+constexpr int kXentSms = 148;        // a wrong guess costs speed, nothing else: results do not change with the device
+constexpr int kMaxSplits = 32;
+constexpr double kItemCost = 12.0, kWholeCost = 4.0;
+constexpr size_t kPartBytes = (size_t)256 << 20;   // at most, per product
+
+double xent_makespan(int64_t n0, double c0, int64_t n1, double c1, int64_t workers) {
+    const int64_t a0 = n0 / workers, e0 = n0 % workers, a1 = n1 / workers, e1 = n1 % workers;
+    const double base = a0 * c0 + a1 * c1;
+    if (e0 + e1 > workers) return base + c0 + c1;   // some worker has one more of both
+    return base + (e0 && c0 > c1 ? c0 : e1 ? (e0 && c0 > c1 ? c0 : c1) : e0 ? c0 : 0.0);
+}
+
+void xent_cut(int64_t dh_tiles, int64_t dh_rounds, int64_t dw_tiles, int64_t dw_rounds, int cg, int* dh_per, int* dw_per) {
+    const int64_t workers = kXentSms / cg;
+    const size_t tile_bytes = (size_t)kTileM * cg * kTileN * sizeof(float);
+    double best = 1e300;
+    for (int sh = 1; sh <= kMaxSplits && (sh == 1 || (dh_rounds >= 8 * sh && sh * dh_tiles * tile_bytes <= kPartBytes)); ++sh)
+        for (int sw = 1; sw <= kMaxSplits && (sw == 1 || (dw_rounds >= 8 * sw && sw * dw_tiles * tile_bytes <= kPartBytes)); ++sw) {
+            const int64_t ph = ceil_div(dh_rounds, sh), pw = ceil_div(dw_rounds, sw);
+            const double t = xent_makespan(dh_tiles * ceil_div(dh_rounds, ph), ph + (sh > 1 ? kItemCost : kWholeCost),
+                                           dw_tiles * ceil_div(dw_rounds, pw), pw + (sw > 1 ? kItemCost : kWholeCost), workers);
+            if (t < best) {
+                best = t;
+                *dh_per = (int)ph;
+                *dw_per = (int)pw;
+            }
+        }
+}
 
 bool xent_sizes_ok(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type) {
     if (tokens < 0 || tokens > (1 << 24) || vocab < 1 || vocab > (1 << 26) || dim < 1 || dim > (1 << 20)) return false;
@@ -268,6 +307,7 @@ XentLayout xent_layout(int64_t tokens, int64_t vocab, int64_t dim, int in_type, 
     L.pack = in_type == TK_F32 || !aligned_rows;
     L.ld = (int)((dim + 7) / 8 * 8);
     L.tiles_v = (int)((vocab + kTileN - 1) / kTileN);
+    L.cg = tokens > kTileM ? 2 : 1;
     size_t at = 0;
     auto take = [&](size_t n) {
         size_t o = at;
@@ -280,7 +320,7 @@ XentLayout xent_layout(int64_t tokens, int64_t vocab, int64_t dim, int in_type, 
     }
     const size_t inputs = at;
     // the loss's own scratch and the gradient's are never alive together
-    L.off_partial = take((size_t)L.tiles_v * tokens * sizeof(float2));
+    L.off_partial = take((size_t)2 * L.tiles_v * tokens * sizeof(float2));
     L.off_picked = take((size_t)tokens * sizeof(float));
     const size_t loss_end = at;
     at = inputs;
@@ -294,21 +334,45 @@ XentLayout xent_layout(int64_t tokens, int64_t vocab, int64_t dim, int in_type, 
         L.piece = ((all + pieces - 1) / pieces + kTileN - 1) / kTileN * kTileN;
         L.off_d = take(row * L.piece);
         L.off_acc = take((size_t)tokens * dim * sizeof(float));
+        const int rows = kTileM * L.cg, pairs = xent_pairs(L.d_parts, L.in_parts);
+        const int64_t across = ceil_div(dim, kTileN), dh_tiles = ceil_div(tokens, rows) * across, dw_tiles = ceil_div(L.piece, rows) * across;
+        const int64_t dh_rounds = ceil_div(L.piece < vocab ? L.piece : vocab, kTileK) * pairs, dw_rounds = ceil_div(tokens > 0 ? tokens : 1, kTileK) * pairs;
+        xent_cut(dh_tiles, dh_rounds, dw_tiles, dw_rounds, L.cg, &L.dh_per, &L.dw_per);
+        const size_t tile_bytes = (size_t)rows * kTileN * sizeof(float);
+        if (L.dh_per < dh_rounds) L.off_dh_part = take(ceil_div(dh_rounds, L.dh_per) * dh_tiles * tile_bytes);
+        if (L.dw_per < dw_rounds) L.off_dw_part = take(ceil_div(dw_rounds, L.dw_per) * dw_tiles * tile_bytes);
     }
     if (at < loss_end) at = loss_end;
     L.bytes = at + 256;
     return L;
 }
 
-// A matrix of `rows` rows of `cols` bf16 values, `parts` of them one after the other, in boxes of 64 x box_rows
-int make_map(Device* d, CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t stride, int parts, int box_rows) {
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
-    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * (cuuint64_t)rows};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
-    CUresult rc = d->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, step,
+int encode(Device* d, CUtensorMap* map, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    const cuuint32_t step[4] = {1, 1, 1, 1};
+    CUresult rc = d->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims, strides, box, step,
                             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return rc == CUDA_SUCCESS ? TK_OK : TK_ERR_CUDA;
+}
+
+// A matrix of `rows` rows of `cols` bf16 values, `parts` of them one after the other, in boxes of 64 x box_rows x box_parts
+int make_map(Device* d, CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t stride, int parts, int box_rows,
+             int box_parts = 1) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_parts};
+    return encode(d, map, p, 3, dims, strides, box);
+}
+
+// The right operand of a gradient product, rows of K: in panels of 64 columns if every tile's share of a CTA starts on one (then no
+// box reaches past a row's end into the next), else in boxes of 64 columns wherever they start
+int make_right_map(Device* d, XentProblem& q, const void* p, int64_t cols, int64_t rows, int64_t stride, int parts, int cg) {
+    q.b_panels = cols % (64 * cg) == 0;
+    if (!q.b_panels) return make_map(d, &q.b, p, cols, rows, stride, parts, 64);
+    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)cols / 64, (cuuint64_t)parts};
+    const cuuint64_t strides[3] = {(cuuint64_t)stride * 2, 128, (cuuint64_t)stride * 2 * (cuuint64_t)rows};
+    const cuuint32_t box[4] = {64, 64, (cuuint32_t)(kTileN / cg / 64), 1};
+    return encode(d, &q.b, p, 4, dims, strides, box);
 }
 
 // A product's part pairs by rising size: all pairs when one side is a single part, else those of order <= 2
@@ -353,7 +417,7 @@ int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
         }
         ready[dev] = true;
     }
-    const u32 workers = a.tiles < (u32)pairs[dev] ? a.tiles : (u32)pairs[dev];
+    const u32 workers = a.items < (u32)pairs[dev] ? a.items : (u32)pairs[dev];
     cfg.gridDim = dim3(workers * CG);
     if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
         cudaGetLastError();
@@ -362,11 +426,31 @@ int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
     return TK_OK;
 }
 
+template <int MODE, int PARTS>
+int launch_xent(Device* d, int cg, const XentArgs& a, cudaStream_t s) {
+    return cg == 2 ? launch_xent<MODE, 2, PARTS>(d, a, s) : launch_xent<MODE, 1, PARTS>(d, a, s);
+}
+
 template <typename T, int PARTS>
 int launch_pack(Device* d, const void* x, int64_t stride, int64_t rows, int64_t dim, int ld, void* out, cudaStream_t s) {
-    const int64_t ctas = (rows * ld + 255) / 256, most = (int64_t)d->sms * 32;
+    const int64_t ctas = ceil_div(rows * ld, 256), most = (int64_t)d->sms * 32;
     if (ctas == 0) return TK_OK;
     xent_pack_kernel<T, PARTS><<<(unsigned)(ctas < most ? ctas : most), 256, 0, s>>>((const T*)x, stride, rows, (int)dim, ld, (bf16*)out);
+    return launch_error();
+}
+
+// The product's rounds in items of at most `per` (0: all), those in accumulation chunks of equal length, at most `most`
+// rounds (0: all).
+void set_rounds(XentProblem& p, int per, int most) {
+    p.rounds = p.kblocks * p.nseg;
+    p.per = per && per < p.rounds ? per : p.rounds;
+    p.splits = (int)ceil_div(p.rounds, p.per);
+    p.chunk = most ? (int)ceil_div(p.per, ceil_div(p.per, most)) : p.per;
+}
+
+int launch_join_tiles(const XentProblem& p, int rows, cudaStream_t s) {
+    if (p.splits == 1) return TK_OK;
+    xent_join_tiles_kernel<<<dim3((unsigned)(p.tiles_m * p.tiles_n), kJoinSlices), 256, 0, s>>>(p, rows);
     return launch_error();
 }
 
@@ -422,29 +506,30 @@ int tk_xent_loss(const void* h, int64_t h_stride, const void* w, int64_t w_strid
     XentInputs in;
     rc = xent_inputs(d, L, h, h_stride, w, w_stride, in_type, tokens, vocab, dim, ws, &in, s);
     if (rc != TK_OK) return rc;
-    constexpr int CG = 1;
     XentArgs a = {};
     XentProblem& p = a.p[0];
     rc = make_map(d, &p.a, in.h, dim, tokens, in.h_stride, L.in_parts, kTileM);
-    if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / CG);
+    if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / L.cg);
     if (rc != TK_OK) return rc;
-    p.tiles_m = (int)((tokens + kTileM * CG - 1) / (kTileM * CG));
+    p.tiles_m = (int)ceil_div(tokens, kTileM * L.cg);
     p.tiles_n = L.tiles_v;
     p.kblocks = (int)((dim + kTileK - 1) / kTileK);
     p.cols = (int)vocab;
     set_segments(p, L.in_parts, L.in_parts);
+    set_rounds(p, 0, kChunk);
     if ((int64_t)p.tiles_m * p.tiles_n >= ((int64_t)1 << 31)) return TK_ERR_INVALID;
-    a.tiles0 = a.tiles = (u32)(p.tiles_m * p.tiles_n);
+    a.items0 = a.items = (u32)(p.tiles_m * p.tiles_n);
     a.tokens = (int)tokens, a.vocab = (int)vocab, a.target = target;
     a.partial = (float2*)(ws + L.off_partial);
     a.picked = (float*)(ws + L.off_picked);
     a.status = d->status;
-    rc = launch_xent<kXentLoss, CG, 1>(d, a, s);
+    rc = launch_xent<kXentLoss, 1>(d, L.cg, a, s);
     if (rc != TK_OK) return rc;
-    // few rows: many lanes per row; from 32 rows a warp on, the loads of a warp are whole lines with one lane each
-    const int lanes = tokens >= 8192 ? 1 : (tokens >= 1024 ? 4 : 32);
+    // few rows: a warp per row; else 8 lanes per row, whose loads are whole sectors (one lane per row took 65 us for 8192 rows
+    // of 394 half tiles, a chain of loads)
+    const int lanes = tokens >= 512 ? 8 : 32;
     const int64_t warps = (tokens + 32 / lanes - 1) / (32 / lanes);
-    xent_join_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a.partial, a.picked, target, (int)tokens, (int)vocab, L.tiles_v, lanes,
+    xent_join_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a.partial, a.picked, target, (int)tokens, (int)vocab, 2 * L.tiles_v, lanes,
                                                                  loss, lse);
     return launch_error();
 }
@@ -477,45 +562,49 @@ int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_strid
     XentInputs in;
     rc = xent_inputs(d, L, h, h_stride, w, w_stride, in_type, tokens, vocab, dim, ws, &in, s);
     if (rc != TK_OK) return rc;
-    constexpr int CG = 1;
-    const int grad_rows = kTileM * CG;
+    const int grad_rows = kTileM * L.cg, panels = (int)(L.piece / 64);
+    const int fine = grad_type == TK_F32 ? kChunk : 0;
     XentArgs soft = {}, grad = {};
     {
         XentProblem& p = soft.p[0];
         rc = make_map(d, &p.a, in.h, dim, tokens, in.h_stride, L.in_parts, kTileM);
-        if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / CG);
-        if (rc == TK_OK) rc = make_map(d, &soft.store, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, 32);
+        if (rc == TK_OK) rc = make_map(d, &p.b, in.w, dim, vocab, in.w_stride, L.in_parts, kTileN / L.cg);
+        if (rc == TK_OK) rc = make_map(d, &soft.store, ws + L.off_d, 64, tokens, 64, panels * L.d_parts, 32);
         if (rc != TK_OK) return rc;
         p.tiles_m = (int)((tokens + grad_rows - 1) / grad_rows);
         p.kblocks = (int)((dim + kTileK - 1) / kTileK);
         p.cols = (int)vocab;
         set_segments(p, L.in_parts, L.in_parts);
+        set_rounds(p, 0, fine);
         soft.tokens = (int)tokens, soft.vocab = (int)vocab, soft.target = target, soft.lse = lse, soft.dloss = dloss;
         soft.status = grad.status = d->status;
+        soft.panels = grad.panels = panels;
         grad.tokens = (int)tokens, grad.vocab = (int)vocab;
     }
     XentProblem pw = {}, ph = {};
     if (dw) {   // dw[v][:] = sum over tokens of D[t][v] h[t][:]
-        rc = make_map(d, &pw.a, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, 64);
-        if (rc == TK_OK) rc = make_map(d, &pw.b, in.h, dim, tokens, in.h_stride, L.in_parts, 64);
+        rc = make_map(d, &pw.a, ws + L.off_d, 64, tokens, 64, panels * L.d_parts, 64, 2);
+        if (rc == TK_OK) rc = make_right_map(d, pw, in.h, dim, tokens, in.h_stride, L.in_parts, L.cg);
         if (rc != TK_OK) return rc;
-        pw.a_mn = pw.b_mn = 1;
+        pw.a_mn = 1;
         pw.tiles_n = (int)((dim + kTileN - 1) / kTileN);
         pw.kblocks = (int)((tokens + kTileK - 1) / kTileK);
         pw.cols = (int)dim;
         set_segments(pw, L.d_parts, L.in_parts);
+        set_rounds(pw, L.dw_per, fine);
+        pw.part = (float*)(ws + L.off_dw_part);
         pw.ld = dw_stride, pw.out_bf16 = grad_type == TK_BF16;
     }
     if (dh) {   // dh[t][:] = sum over the vocabulary of D[t][v] w[v][:]
-        rc = make_map(d, &ph.a, ws + L.off_d, L.piece, tokens, L.piece, L.d_parts, kTileM);
-        if (rc == TK_OK) rc = make_map(d, &ph.b, in.w, dim, vocab, in.w_stride, L.in_parts, 64);
+        rc = make_map(d, &ph.a, ws + L.off_d, 64, tokens, 64, panels * L.d_parts, kTileM);
+        if (rc == TK_OK) rc = make_right_map(d, ph, in.w, dim, vocab, in.w_stride, L.in_parts, L.cg);
         if (rc != TK_OK) return rc;
-        ph.b_mn = 1;
         ph.tiles_m = soft.p[0].tiles_m;
         ph.tiles_n = (int)((dim + kTileN - 1) / kTileN);
         ph.cols = (int)dim;
         set_segments(ph, L.d_parts, L.in_parts);
         ph.acc = (float*)(ws + L.off_acc);
+        ph.part = (float*)(ws + L.off_dh_part);
         ph.ld = dh_stride, ph.rows = tokens, ph.out_bf16 = grad_type == TK_BF16;
     }
     for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
@@ -525,29 +614,30 @@ int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_strid
         p.tiles_n = (int)((here + kTileN - 1) / kTileN);
         p.b_off = (int)v0;
         soft.v0 = (int)v0;
-        soft.tiles0 = soft.tiles = (u32)(p.tiles_m * p.tiles_n);
-        rc = L.d_parts == 1 ? launch_xent<kXentSoft, CG, 1>(d, soft, s) : launch_xent<kXentSoft, CG, 3>(d, soft, s);
+        soft.items0 = soft.items = (u32)(p.tiles_m * p.tiles_n);
+        rc = L.d_parts == 1 ? launch_xent<kXentSoft, 1>(d, L.cg, soft, s) : launch_xent<kXentSoft, 3>(d, L.cg, soft, s);
         if (rc != TK_OK) return rc;
         int n = 0;
-        grad.tiles0 = grad.tiles = 0;
-        u32 tiles[2] = {0, 0};
+        u32 items[2] = {0, 0};
         if (dh) {
-            ph.kblocks = (int)((here + kTileK - 1) / kTileK);
+            ph.kblocks = (int)ceil_div(here, kTileK);
             ph.b_koff = (int)v0;
             ph.acc_read = !first, ph.acc_write = !last;
             ph.out = last ? dh : nullptr;
-            tiles[n] = (u32)(ph.tiles_m * ph.tiles_n);
+            set_rounds(ph, L.dh_per, fine);
+            items[n] = (u32)(ph.tiles_m * ph.tiles_n * ph.splits);
             grad.p[n++] = ph;
         }
         if (dw) {
-            pw.tiles_m = (int)((here + grad_rows - 1) / grad_rows);
+            pw.tiles_m = (int)ceil_div(here, grad_rows);
             pw.rows = here;
             pw.out = (char*)dw + v0 * dw_stride * e;
-            tiles[n] = (u32)(pw.tiles_m * pw.tiles_n);
+            items[n] = (u32)(pw.tiles_m * pw.tiles_n * pw.splits);
             grad.p[n++] = pw;
         }
-        grad.tiles0 = tiles[0], grad.tiles = tiles[0] + tiles[1];
-        rc = launch_xent<kXentGrad, CG, 1>(d, grad, s);
+        grad.items0 = items[0], grad.items = items[0] + items[1];
+        rc = launch_xent<kXentGrad, 1>(d, L.cg, grad, s);
+        for (int i = 0; i < n && rc == TK_OK; ++i) rc = launch_join_tiles(grad.p[i], grad_rows, s);
         if (rc != TK_OK) return rc;
     }
     return TK_OK;

@@ -19,7 +19,13 @@
 //
 // One CTA (CG 1) or pair (CG 2) per SM (pair) is persistent over tiles of 128 CG x 256: one thread issues TMA
 // loads into a ring of stages of 64 of K, one issues the matrix instructions into one of two accumulators
-// of 256 columns of tensor memory, four warps take the other accumulator to its destination meanwhile.
+// of 256 columns of tensor memory, eight warps take the other to registers, 128 columns of a row per thread,
+// give it back at once and carry the values to their destination meanwhile.
+//
+// The accumulators of the matrix instructions truncate: every 16 products cost up to half a unit in the last place of the running
+// sum, always towards zero (measured: 2e-8 of a sum per 16 products, 1.2e-5 over 10,007 of them).  Results that
+// are to be good to fp32 are therefore summed in chunks of at most kChunk blocks of 64 products, added
+// up in registers with correct rounding.
 // Both gradient products read D or w or h along the dimension that is not contiguous; the matrix
 // instructions take such operands ("MN-major") directly, so nothing is transposed in memory.
 #pragma once
@@ -31,44 +37,57 @@ namespace tk {
 enum { kXentLoss = 0, kXentSoft = 1, kXentGrad = 2 };
 
 constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
-constexpr int kXentThreads = 256;   // warps: TMA, matrix instructions, tensor memory, -, 4 x epilogue
-constexpr int kXentEpiWarp = 4;
+constexpr int kXentThreads = 384;   // warps: TMA, matrix instructions, tensor memory, -, 8 x epilogue
+constexpr int kXentEpiWarp = 4, kXentEpiWarps = 8;
+constexpr int kEpiCols = 128;       // columns an epilogue thread holds
+// Blocks of 64 products summed in tensor memory where fp32 accuracy is wanted: in the loss and in the products of fp32 gradients.
+// Loss and gradient take the same, so that what truncation is left in l cancels in exp(l - lse).
+constexpr int kChunk = 8;
 constexpr int kBoxBytes = 64 * 64 * 2;                        // an MN-major box: 64 values x 64 of K
 constexpr int kABytes = kTileM * kTileK * 2;
 template <int CG> struct XentShape {
     static constexpr int kBRows = kTileN / CG;                // rows of the right operand this CTA holds
     static constexpr int kStageBytes = kABytes + kBRows * kTileK * 2;
     static constexpr int kStages = CG == 1 ? 4 : 6;           // 192 KB either way
-    static constexpr int kStaging = 8192;                     // per epilogue warp
-    static constexpr int kSmem = kStages * kStageBytes + 4 * kStaging + 512 + 1024;
+    static constexpr int kStaging = 4096;                     // per epilogue warp
+    static constexpr int kSmem = kStages * kStageBytes + kXentEpiWarps * kStaging + 512 + 1024;
 };
 
 struct alignas(64) XentProblem {
     CUtensorMap a, b;
     int tiles_m, tiles_n, kblocks;
+    int rounds;               // K blocks times part pairs
+    int chunk;                // rounds per accumulation in tensor memory
+    int splits, per;          // kGrad: a tile's rounds are cut into `splits` items of `per` rounds (the last may be shorter)
     int cols;                 // columns of the result
-    int a_mn, b_mn;           // operand is MN-major
+    int a_mn;                 // kGrad: A is MN-major (dw); B always is
+    int b_panels;             // kGrad: B's map is in panels of 64 columns and one load brings all of a stage's (rows of whole panels)
     int a_off, b_off;         // first row (M, N) within the operand's map
     int a_koff, b_koff;       // first K within the operand's map
     int nseg;                 // part pairs, smallest products first
     unsigned char sa[6], sb[6];
     // kGrad: where the tile goes
     void* out;                // null: only into acc
-    float* acc;               // fp32 [rows][cols], or null
+    float* acc;               // fp32 [rows][cols]: the sum over the pieces so far
+    float* part;              // splits > 1: [splits][tiles][128 CG][256] sums, joined by xent_join_tiles_kernel
     int64_t ld, rows;
     int out_bf16, acc_read, acc_write;
 };
 
 struct XentArgs {
     XentProblem p[2];
-    CUtensorMap store;        // kSoft: D, [parts][tokens][piece]
-    u32 tiles0, tiles;        // tiles of the first problem, and of both
+    // D of a piece lies in panels of 64 vocabulary entries, [parts][piece / 64][tokens][64]: every tile that a TMA
+    // instruction stores or loads is one contiguous stretch of 4 to 16 KB, whichever product reads it
+    // (as [tokens][piece], the loads were 128-byte pieces of rows 25 KB apart).
+    CUtensorMap store;
+    int panels;               // piece / 64
+    u32 items0, items;        // items of the first problem (kGrad: dh), and of both
     int tokens, vocab;
     int v0;                   // kSoft: first vocabulary entry of the piece
     const int* target;
     const float* lse;
     const float* dloss;
-    float2* partial;          // kLoss: [tile of the vocabulary][tokens] (maximum, sum)
+    float2* partial;          // kLoss: [half tile of the vocabulary][tokens] (maximum, sum)
     float* picked;            // kLoss: [tokens] logit of the target
     int* status;
 };
@@ -92,20 +111,36 @@ __device__ __forceinline__ float exp2_gradual(float x) {
 // 2^-20 of the result, far below bf16's; the three-part form subtracts lse first instead.)
 constexpr float kSoftLift = 24.0f, kSoftDrop = 5.9604644775390625e-8f;
 
-struct XentTile {
+struct XentItem {
     int problem, m, n;
+    int r0, r1;      // rounds [r0, r1) of the tile: round r is K block r % kblocks of part pair r / kblocks
+    int split;
 };
-template <int MODE> __device__ __forceinline__ XentTile xent_tile(const XentArgs& A, u32 id) {
-    XentTile t;
-    t.problem = id >= A.tiles0;
+
+// The items of a launch go to its workers in turn.  kLoss, kSoft: tiles, all tokens against the same part of w before
+// the next.  kGrad: the items of dh, then of dw; the tiles of one row of the result, which share the long operand D, side by
+// side, and the same rounds of all tiles before the next.  Workers then move through K in step, and D, w and h come
+// from DRAM about once.  (An equal stretch of all rounds per worker balances better still, but its workers are
+// at different places of K: 8192 x 50257 x 768 read 1.13 GB per launch instead of 0.50 and took the same
+// time, 4096 x 131072 x 2048 took 12 % longer.)  What the splits are for is evening out the workers: see train.cu.
+template <int MODE> __device__ __forceinline__ XentItem xent_item(const XentArgs& A, u32 id) {
+    XentItem t;
+    t.problem = MODE == kXentGrad && id >= A.items0;
+    if (t.problem) id -= A.items0;
     const XentProblem& P = A.p[t.problem];
-    if (t.problem) id -= A.tiles0;
-    if (MODE == kXentGrad) {   // the tiles of a row of the result share the long operand: side by side
-        t.m = (int)(id / (u32)P.tiles_n);
-        t.n = (int)(id % (u32)P.tiles_n);
-    } else {                   // all tokens meet the same part of w before the next
+    if (MODE == kXentGrad) {
+        const u32 tiles = (u32)(P.tiles_m * P.tiles_n), tile = id % tiles;
+        t.split = (int)(id / tiles);
+        t.m = (int)(tile / (u32)P.tiles_n);
+        t.n = (int)(tile % (u32)P.tiles_n);
+        t.r0 = t.split * P.per;
+        t.r1 = min(t.r0 + P.per, P.rounds);
+    } else {
+        t.split = 0;
         t.m = (int)(id % (u32)P.tiles_m);
         t.n = (int)(id / (u32)P.tiles_m);
+        t.r0 = 0;
+        t.r1 = P.rounds;
     }
     return t;
 }
@@ -113,25 +148,6 @@ template <int MODE, int CG> __device__ __forceinline__ int xent_columns(const Xe
     if (MODE != kXentGrad) return kTileN;
     const int left = P.cols - n * kTileN, unit = 16 * CG;
     return left >= kTileN ? kTileN : (left + unit - 1) / unit * unit;
-}
-
-// One row's 32 logits into the running (maximum, sum of exp2((l - maximum) log2 e)).
-__device__ __forceinline__ void loss_chunk(const float (&v)[32], float& top, float& sum) {
-    float t = fmaxf(v[0], v[1]);
-#pragma unroll
-    for (int i = 2; i < 32; ++i) t = fmaxf(t, v[i]);
-    if (t > top) {
-        sum *= exp2_approx((top - t) * kLog2e);
-        top = t;
-    }
-    const float shift = top * kLog2e;
-    float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        s0 += exp2_approx(fmaf(v[i], kLog2e, -shift));
-        s1 += exp2_approx(fmaf(v[i + 1], kLog2e, -shift));
-    }
-    sum += s0 + s1;
 }
 
 // Two values' part `p` as a word of two bf16, leaving in a, b what the parts so far do not hold
@@ -151,7 +167,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
     const u32 base = (smem_addr(raw) + 1023u) & ~1023u;
     unsigned char* sm = raw + (base - smem_addr(raw));
     const u32 staging = base + S::kStages * S::kStageBytes;
-    const u32 bars = staging + 4 * S::kStaging;
+    const u32 bars = staging + kXentEpiWarps * S::kStaging;
     const u32 full = bars, empty = bars + 8 * S::kStages, done = bars + 16 * S::kStages, freed = done + 16, drain = done + 32;
     const u32 tmem_slot = done + 48;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -165,7 +181,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(done + 8 * i, 1);
-            mbar_init(freed + 8 * i, 4 * CG);
+            mbar_init(freed + 8 * i, kXentEpiWarps * CG);
         }
         mbar_init(drain, 1);
         mbar_init_fence();
@@ -177,37 +193,52 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
     tcgen05_fence_after();
     const u32 tmem = *(volatile u32*)(sm + (tmem_slot - base));
 
+    // 384 threads x 168 registers at launch; the epilogue's two warpgroups take over what the first gives up
+    // (128 x 56 + 256 x 216 = 62,464 of 64,512)
+    if (warp < kXentEpiWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 && lane == 0) {
         // ---- loads ----
         const u32 full0 = CG == 2 ? mapped_addr(full, 0) : full;   // both CTAs' copies report to the leader
         u32 it = 0;
         bool ok = true;
-        for (u32 id = worker; ok && id < A.tiles; id += workers) {
-            const XentTile t = xent_tile<MODE>(A, id);
+        for (u32 id = worker; ok && id < A.items; id += workers) {
+            const XentItem t = xent_item<MODE>(A, id);
             const XentProblem& P = A.p[t.problem];
             const int mine = xent_columns<MODE, CG>(P, t.n) / CG;
             const int a0 = P.a_off + (t.m * CG + (int)rank) * kTileM, b0 = P.b_off + t.n * kTileN + (int)rank * mine;
-            const int boxes = P.b_mn ? (mine + 63) / 64 : 0;
-            const u32 bytes = kABytes + (P.b_mn ? boxes * kBoxBytes : S::kBRows * kTileK * 2);
-            for (int s = 0; ok && s < P.nseg; ++s) {
-                const int pa = P.sa[s], pb = P.sb[s];
-                for (int k = 0; k < P.kblocks; ++k, ++it) {
+            const int boxes = MODE == kXentGrad ? (P.b_panels ? S::kBRows / 64 : (mine + 63) / 64) : 0;
+            const u32 bytes = kABytes + (MODE == kXentGrad ? boxes * kBoxBytes : S::kBRows * kTileK * 2);
+            // the loop below has half a microsecond per round: nothing of it is looked up in the parameters
+            const int kblocks = P.kblocks, a_koff = P.a_koff, b_koff = P.b_koff, a_mn = P.a_mn, b_panels = P.b_panels, panels = A.panels;
+            const CUtensorMap *map_a = &P.a, *map_b = &P.b;
+            int seg = t.r0 / kblocks, k = t.r0 % kblocks;
+            for (int r = t.r0; r < t.r1;) {
+                const int pa = P.sa[seg], pb = P.sb[seg];
+                ++seg;
+                for (; k < kblocks && r < t.r1; ++k, ++r, ++it) {
                     const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
                     if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1))) break;
                     const u32 a = base + stage * S::kStageBytes, b = a + kABytes, bar = full0 + 8 * stage;
                     if (rank == 0) mbar_expect(full + 8 * stage, bytes * CG);
-                    const int ka = P.a_koff + k * kTileK, kb = P.b_koff + k * kTileK;
-                    if (P.a_mn) {
-                        tma_load<CG>(a, &P.a, bar, a0, ka, pa);
-                        tma_load<CG>(a + kBoxBytes, &P.a, bar, a0 + 64, ka, pa);
+                    const int ka = a_koff + k * kTileK, kb = b_koff + k * kTileK;
+                    if (MODE != kXentGrad) {
+                        tma_load<CG>(a, map_a, bar, ka, a0, pa);
+                        tma_load<CG>(b, map_b, bar, kb, b0, pb);
                     } else {
-                        tma_load<CG>(a, &P.a, bar, ka, a0, pa);
+                        if (a_mn) {   // D: panels of 64 vocabulary entries
+                            tma_load<CG>(a, map_a, bar, 0, ka, a0 / 64 + pa * panels);
+                        } else {
+                            tma_load<CG>(a, map_a, bar, 0, a0, k + pa * panels);
+                        }
+                        if (b_panels)
+                            tma_load4<CG>(b, map_b, bar, 0, kb, b0 / 64, pb);
+                        else
+                            for (int j = 0; j < boxes; ++j) tma_load<CG>(b + j * kBoxBytes, map_b, bar, b0 + 64 * j, kb, pb);
                     }
-                    if (P.b_mn)
-                        for (int j = 0; j < boxes; ++j) tma_load<CG>(b + j * kBoxBytes, &P.b, bar, b0 + 64 * j, kb, pb);
-                    else
-                        tma_load<CG>(b, &P.b, bar, kb, b0, pb);
                 }
+                if (!ok) break;
+                k = 0;
             }
         }
         // nothing of this CTA is in flight when it ends: every stage that was filled has been consumed
@@ -218,45 +249,52 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
         // ---- matrix instructions ----
         u32 it = 0, turn = 0;
         bool ok = true;
-        for (u32 id = worker; ok && id < A.tiles; id += workers, ++turn) {
-            const XentTile t = xent_tile<MODE>(A, id);
+        for (u32 id = worker; ok && id < A.items; id += workers) {
+            const XentItem t = xent_item<MODE>(A, id);
             const XentProblem& P = A.p[t.problem];
-            const u32 desc = mma_desc(kTileM * CG, xent_columns<MODE, CG>(P, t.n), P.a_mn, P.b_mn);
-            const u32 slot = turn & 1, acc = tmem + slot * kTileN;
-            if (!(ok = mbar_wait(freed + 8 * slot, ((turn >> 1) & 1) ^ 1))) break;
-            tcgen05_fence_after();
-            const u64 step_a = P.a_mn ? 2048 >> 4 : 32 >> 4, step_b = P.b_mn ? 2048 >> 4 : 32 >> 4;
-            const int rounds = P.nseg * P.kblocks;
-            for (int k = 0; k < rounds; ++k, ++it) {
-                const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
-                if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+            const bool a_mn = MODE == kXentGrad && P.a_mn, b_mn = MODE == kXentGrad;
+            const u32 desc = mma_desc(kTileM * CG, xent_columns<MODE, CG>(P, t.n), a_mn, b_mn);
+            const u64 step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4;
+            const u64 first_a = smem_desc(base, a_mn ? kBoxBytes : 0, 1024), first_b = smem_desc(base + kABytes, b_mn ? kBoxBytes : 0, 1024);
+            const int rounds = t.r1 - t.r0, chunk = P.chunk;
+            for (int r0 = 0; ok && r0 < rounds; r0 += chunk, ++turn) {
+                const u32 slot = turn & 1, acc = tmem + slot * kTileN;
+                if (!(ok = mbar_wait(freed + 8 * slot, ((turn >> 1) & 1) ^ 1))) break;
                 tcgen05_fence_after();
-                const u32 a = base + stage * S::kStageBytes, b = a + kABytes;
-                u64 da = smem_desc(a, P.a_mn ? kBoxBytes : 0, 1024), db = smem_desc(b, P.b_mn ? kBoxBytes : 0, 1024);
+                const int n = min(chunk, rounds - r0);
+                for (int k = 0; k < n; ++k, ++it) {
+                    const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
+                    if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+                    tcgen05_fence_after();
+                    const u64 da = first_a + stage * (S::kStageBytes >> 4), db = first_b + stage * (S::kStageBytes >> 4);
 #pragma unroll
-                for (int i = 0; i < kTileK / 16; ++i) mma_bf16<CG>(acc, da + i * step_a, db + i * step_b, desc, k > 0 || i > 0);
-                mma_commit<CG>(empty + 8 * stage);
+                    for (int i = 0; i < kTileK / 16; ++i) mma_bf16<CG>(acc, da + i * step_a, db + i * step_b, desc, k > 0 || i > 0);
+                    mma_commit<CG>(empty + 8 * stage);
+                }
+                if (ok) mma_commit<CG>(done + 8 * slot);
             }
-            if (ok) mma_commit<CG>(done + 8 * slot);
         }
         if (!ok) {
             mma_commit<CG>(drain);
             mbar_wait(drain, 0);
             atomicExch(A.status, 1);
         }
-    } else if (warp >= kXentEpiWarp) {
+    }
+    } else {
         // ---- accumulators to their destination ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int w = warp - kXentEpiWarp;
+        const int quarter = w & 3, half = w >> 2;    // rows (a warp reaches the tensor memory lanes of its rank modulo 4), columns
         const u32 stage_smem = staging + w * S::kStaging;
         float* stage_ptr = (float*)(sm + (stage_smem - base));
-        const u32 freed0 = CG == 2 ? mapped_addr(freed, 0) : mapped_addr(freed, cluster_rank());
+        const u32 freed0 = mapped_addr(freed, CG == 2 ? 0 : cluster_rank());
         u32 turn = 0;
-        for (u32 id = worker; id < A.tiles; id += workers, ++turn) {
-            const XentTile t = xent_tile<MODE>(A, id);
+        bool ok = true;
+        for (u32 id = worker; id < A.items; id += workers) {
+            const XentItem t = xent_item<MODE>(A, id);
             const XentProblem& P = A.p[t.problem];
-            const u32 slot = turn & 1;
-            const int m0 = (t.m * CG + (int)rank) * kTileM + 32 * w;   // first row of this warp
-            const int row = m0 + lane, n0 = t.n * kTileN;
+            const int m0 = (t.m * CG + (int)rank) * kTileM + 32 * quarter;   // first row of this warp
+            const int row = m0 + lane, n0 = t.n * kTileN + half * kEpiCols;  // first column
             int target = -1;
             float scale = 0.0f, lse = 0.0f;
             if (MODE != kXentGrad && row < A.tokens) {
@@ -266,138 +304,221 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                     scale = target >= 0 && target < A.vocab ? A.dloss[row] : 0.0f;
                 }
             }
-            if (!mbar_wait(done + 8 * slot, (turn >> 1) & 1)) {
+            float v[kEpiCols];
+            const int rounds = t.r1 - t.r0, chunk = P.chunk;
+            for (int r0 = 0; r0 < rounds; r0 += chunk, ++turn) {
+                const u32 slot = turn & 1;
+                if (!(ok = mbar_wait(done + 8 * slot, (turn >> 1) & 1))) break;
+                tcgen05_fence_after();
+                const u32 acc = tmem + slot * kTileN + half * kEpiCols + ((u32)(32 * quarter) << 16);
+                if (r0 == 0) {
+#pragma unroll
+                    for (int c = 0; c < kEpiCols; c += 32) tmem_load32(acc + c, *(float(*)[32])(v + c));
+                    tmem_load_wait();
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kEpiCols; c += 16) {
+                        float x[16];
+                        tmem_load16(acc + c, x);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[c + i] += x[i];
+                    }
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(freed0 + 8 * slot);
+            }
+            if (!ok) {
                 if (lane == 0) atomicExch(A.status, 1);
                 break;
             }
-            tcgen05_fence_after();
-            const u32 acc = tmem + slot * kTileN + ((u32)(32 * w) << 16);
             if (MODE == kXentLoss) {
-                const int valid = min(kTileN, A.vocab - n0);
-                const int hit = target >= 0 ? target - n0 : -1;   // column of the target, if it is in this tile
+                const int valid = A.vocab - n0;
                 float top = -3.0e38f, sum = 0.0f;
-#pragma unroll 1
-                for (int c = 0; c < valid; c += 32) {
-                    float v[32];
-                    tmem_load32(acc + c, v);
-                    tmem_load_wait();
-                    if (c + 32 > valid) {
+                if (valid > 0) {
+                    const u32 hit = target >= 0 && target < A.vocab ? (u32)(target - n0) : ~0u;   // the target's column, if it is here
+                    if (valid < kEpiCols) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (c + i >= valid) v[i] = -INFINITY;
+                        for (int i = 0; i < kEpiCols; ++i)
+                            if (i >= valid) v[i] = -INFINITY;
                     }
-                    const bool here = (u32)(hit - c) < 32u && hit < valid;
-                    if (__any_sync(0xffffffffu, here)) {
+                    if (__any_sync(0xffffffffu, hit < (u32)kEpiCols)) {
                         float x = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (c + i == hit) x = v[i];
-                        if (here) A.picked[row] = x;
+                        for (int i = 0; i < kEpiCols; ++i)
+                            if ((u32)i == hit) x = v[i];
+                        if (hit < (u32)kEpiCols) A.picked[row] = x;
                     }
-                    loss_chunk(v, top, sum);
+                    float t0 = top, t1 = top, t2 = top, t3 = top;
+#pragma unroll
+                    for (int i = 0; i < kEpiCols; i += 4) {
+                        t0 = fmaxf(t0, v[i]);
+                        t1 = fmaxf(t1, v[i + 1]);
+                        t2 = fmaxf(t2, v[i + 2]);
+                        t3 = fmaxf(t3, v[i + 3]);
+                    }
+                    top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+                    const float shift = top * kLog2e;
+                    float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < kEpiCols; i += 4) {
+                        s0 += exp2_approx(fmaf(v[i], kLog2e, -shift));
+                        s1 += exp2_approx(fmaf(v[i + 1], kLog2e, -shift));
+                        s2 += exp2_approx(fmaf(v[i + 2], kLog2e, -shift));
+                        s3 += exp2_approx(fmaf(v[i + 3], kLog2e, -shift));
+                    }
+                    sum = (s0 + s1) + (s2 + s3);
                 }
-                if (row < A.tokens) A.partial[(int64_t)t.n * A.tokens + row] = make_float2(top, sum);
+                if (row < A.tokens) A.partial[(int64_t)(2 * t.n + half) * A.tokens + row] = make_float2(top, sum);
             } else if (MODE == kXentSoft) {
-                const int valid = min(kTileN, A.vocab - A.v0 - n0);
-                const int hit = target >= 0 ? target - A.v0 - n0 : -1;
-                const float shift = kSoftLift - lse * kLog2e, drop = scale * kSoftDrop;
-#pragma unroll 1
-                for (int c = 0; c < kTileN; c += 64) {
-                    float v[64];
-                    tmem_load32(acc + c, *(float(*)[32])v);
-                    tmem_load32(acc + c + 32, *(float(*)[32])(v + 32));
-                    tmem_load_wait();
-                    if (PARTS == 1) {
+                const int valid = A.vocab - A.v0 - n0;
+                const u32 hit = target >= 0 ? (u32)(target - A.v0 - n0) : ~0u;
+                if (PARTS == 1) {
+                    const float shift = kSoftLift - lse * kLog2e, drop = scale * kSoftDrop;
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) v[i] = drop * exp2_approx(fmaf(v[i], kLog2e, shift));
-                    } else {
+                    for (int i = 0; i < kEpiCols; ++i) v[i] = drop * exp2_approx(fmaf(v[i], kLog2e, shift));
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) v[i] = scale * exp2_gradual((v[i] - lse) * kLog2e);
-                    }
-                    if (c + 64 > valid) {   // past the end of the vocabulary: exact zeros
+                    for (int i = 0; i < kEpiCols; ++i) v[i] = scale * exp2_gradual((v[i] - lse) * kLog2e);
+                }
+                if (valid < kEpiCols) {   // past the end of the vocabulary: exact zeros
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (c + i >= valid) v[i] = 0.0f;
-                    }
-                    if (__any_sync(0xffffffffu, (u32)(hit - c) < 64u)) {
+                    for (int i = 0; i < kEpiCols; ++i)
+                        if (i >= valid) v[i] = 0.0f;
+                }
+                if (__any_sync(0xffffffffu, hit < (u32)kEpiCols)) {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
-                            if (c + i == hit) v[i] -= scale;
-                    }
+                    for (int i = 0; i < kEpiCols; ++i)
+                        if ((u32)i == hit) v[i] -= scale;
+                }
+#pragma unroll
+                for (int c = 0; c < kEpiCols; c += 64)
 #pragma unroll
                     for (int p = 0; p < PARTS; ++p) {
-                        // the buffer's previous store has been read (two buffers, one store each in flight)
-                        const u32 buf = ((c >> 6) * PARTS + p) & 1;
-                        if (lane == 0) tma_store_wait_read<1>();
+                        if (lane == 0) tma_store_wait_read<0>();   // the previous store has left the buffer
                         __syncwarp();
-                        u32* to = (u32*)stage_ptr + buf * 1024 + lane * 32;
+                        u32* to = (u32*)stage_ptr + lane * 32;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             uint4 q;
-                            q.x = take_part(v[8 * j], v[8 * j + 1], p == PARTS - 1);
-                            q.y = take_part(v[8 * j + 2], v[8 * j + 3], p == PARTS - 1);
-                            q.z = take_part(v[8 * j + 4], v[8 * j + 5], p == PARTS - 1);
-                            q.w = take_part(v[8 * j + 6], v[8 * j + 7], p == PARTS - 1);
+                            float* x = v + c + 8 * j;
+                            q.x = take_part(x[0], x[1], p == PARTS - 1);
+                            q.y = take_part(x[2], x[3], p == PARTS - 1);
+                            q.z = take_part(x[4], x[5], p == PARTS - 1);
+                            q.w = take_part(x[6], x[7], p == PARTS - 1);
                             *(uint4*)(to + ((j ^ (lane & 7)) << 2)) = q;
                         }
                         smem_to_async_fence();
                         __syncwarp();
                         if (lane == 0) {
-                            if (m0 < A.tokens) tma_store(&A.store, stage_smem + buf * 4096, n0 + c, m0, p);
+                            if (m0 < A.tokens) tma_store(&A.store, stage_smem, 0, m0, (n0 + c) / 64 + p * A.panels);
                             tma_store_commit();
                         }
                     }
-                }
             } else {
-                const int cols = min(kTileN, P.cols - n0);
-#pragma unroll 1
-                for (int c = 0; c < cols; c += 32) {
-                    float v[32];
-                    tmem_load32(acc + c, v);
-                    tmem_load_wait();
+                const bool whole = P.splits == 1;
+                const int cols = whole ? P.cols - n0 : kEpiCols, rows = whole ? (int)min((int64_t)32, P.rows - m0) : 32;
+                float* sum = whole ? P.acc + (int64_t)m0 * P.cols + n0
+                                   : P.part + (((int64_t)t.split * P.tiles_m + t.m) * P.tiles_n + t.n) * kTileM * CG * kTileN +
+                                         ((int)rank * kTileM + 32 * quarter) * kTileN + half * kEpiCols;
+                const int pitch = whole ? P.cols : kTileN;
+                const bool read = whole && P.acc_read, write = !whole || P.acc_write, out = whole && P.out;
+#pragma unroll
+                for (int c = 0; c < kEpiCols; c += 32) {
                     __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) stage_ptr[lane * 33 + i] = v[i];
+                    for (int i = 0; i < 32; ++i) stage_ptr[lane * 32 + (i ^ lane)] = v[c + i];
                     __syncwarp();
                     if (c + lane < cols) {
-                        const int64_t col = n0 + c + lane;
-                        for (int r = 0; r < 32 && m0 + r < P.rows; ++r) {
-                            float x = stage_ptr[r * 33 + lane];
-                            float* sum = P.acc + (int64_t)(m0 + r) * P.cols + col;
-                            if (P.acc_read) x += *sum;
-                            if (P.acc_write) *sum = x;
-                            if (P.out) store_any(P.out, (int64_t)(m0 + r) * P.ld + col, x, P.out_bf16);
+                        float* to = sum + c + lane;
+                        int64_t at = (int64_t)m0 * P.ld + n0 + c + lane;
+#pragma unroll 4
+                        for (int r = 0; r < rows; ++r, to += pitch, at += P.ld) {
+                            float x = stage_ptr[r * 32 + (lane ^ r)];
+                            if (read) x += *to;
+                            if (write) *to = x;
+                            if (out) store_any(P.out, at, x, P.out_bf16);
                         }
                     }
                 }
             }
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(freed0 + 8 * slot);
         }
         if (MODE == kXentSoft && lane == 0) tma_store_wait_all();
     }
+    __syncwarp();
     tcgen05_fence_before();
     __syncthreads();
     if (CG == 2) cluster_sync();
     if (warp == 2) tmem_free<CG>(tmem, 512);
 }
 
+// Adds up the items of each tile in the order of their rounds, and what the earlier pieces of the vocabulary left.
+constexpr int kJoinSlices = 8;
+__global__ void __launch_bounds__(256) xent_join_tiles_kernel(const __grid_constant__ XentProblem P, int rows) {
+    const int m = blockIdx.x / P.tiles_n, n = blockIdx.x % P.tiles_n;
+    const int quads = rows * kTileN / 4 / kJoinSlices;   // a multiple of 1024
+    const float4* head = (const float4*)(P.part + (int64_t)blockIdx.x * rows * kTileN);
+    const int64_t next_split = (int64_t)gridDim.x * rows * kTileN / 4;
+    for (int i0 = blockIdx.y * quads + threadIdx.x; i0 < (blockIdx.y + 1) * quads; i0 += 1024) {
+        float4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = head[i0 + 256 * j];
+        const float4* next = head;
+        for (int k = 1; k < P.splits; ++k) {
+            next += next_split;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 q = next[i0 + 256 * j];
+                x[j].x += q.x;
+                x[j].y += q.y;
+                x[j].z += q.z;
+                x[j].w += q.w;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 256 * j;
+            const int64_t r = (int64_t)m * rows + i / (kTileN / 4);
+            const int c = n * kTileN + i % (kTileN / 4) * 4;
+            const float y[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (r >= P.rows || c + e >= P.cols) continue;
+                float v = y[e];
+                if (P.acc_read) v += P.acc[r * P.cols + c + e];
+                if (P.acc_write) P.acc[r * P.cols + c + e] = v;
+                if (P.out) store_any(P.out, r * P.ld + c + e, v, P.out_bf16);
+            }
+        }
+    }
+}
+
 // Joins the tiles of each row: lse and loss.  `lanes` (a power of two up to 32) threads per row.
 __global__ void __launch_bounds__(256) xent_join_kernel(const float2* partial, const float* picked, const int* target, int tokens,
                                                         int vocab, int tiles, int lanes, float* loss, float* lse) {
-    // lanes of a warp lie side by side along the rows, so that a warp's loads are whole lines when lanes is 1
+    // the lanes of a warp lie side by side along the rows: four rows make a sector of 32 bytes
     const int rows = 32 / lanes;
     const int warp = (int)((blockIdx.x * 256 + threadIdx.x) >> 5), lane = threadIdx.x & 31;
     const int row = warp * rows + lane % rows;
     float top = -3.0e38f, sum = 0.0f;
-    if (row < tokens)
-        for (int i = lane / rows; i < tiles; i += lanes) {
-            const float2 q = partial[(int64_t)i * tokens + row];
-            const float t = fmaxf(top, q.x);
-            sum = sum * exp2_approx((top - t) * kLog2e) + q.y * exp2_approx((q.x - t) * kLog2e);
+    if (row < tokens) {
+        const float2* at = partial + (int64_t)(lane / rows) * tokens + row;
+        const int64_t step = (int64_t)lanes * tokens;
+        int left = (tiles - lane / rows + lanes - 1) / lanes;
+        for (; left > 0; left -= 8, at += 8 * step) {   // eight loads in flight
+            float2 q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = j < left ? at[j * step] : make_float2(-3.0e38f, 0.0f);
+            float t = top;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t = fmaxf(t, q[j].x);
+            sum *= exp2_approx((top - t) * kLog2e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += q[j].y * exp2_approx((q[j].x - t) * kLog2e);
             top = t;
         }
+    }
     for (int o = rows; o < 32; o <<= 1) {
         const float t2 = __shfl_xor_sync(0xffffffffu, top, o), s2 = __shfl_xor_sync(0xffffffffu, sum, o);
         const float t = fmaxf(top, t2);

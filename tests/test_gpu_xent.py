@@ -100,6 +100,13 @@ def test_more_tiles_than_multiprocessors(dt, gdt):
     run(*make(1500, 9000, 128, dt), gdt)
 
 
+# results 1, 3, 5, 9 and 17 tiles wide: teams of different sizes, tiles cut by the ends of their stretches
+@pytest.mark.parametrize("dt,gdt", TYPES)
+@pytest.mark.parametrize("tokens,vocab,dim", [(2000, 700, 100), (90, 30_000, 600), (700, 3000, 1290), (300, 5000, 2310), (200, 600, 4200)])
+def test_cut_tiles(tokens, vocab, dim, dt, gdt):
+    run(*make(tokens, vocab, dim, dt), gdt)
+
+
 @pytest.mark.parametrize("gdt", [BF16, F32])
 def test_several_pieces(gdt):
     # more columns than one piece of the workspace holds; the last piece ends inside a tile
