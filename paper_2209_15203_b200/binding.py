@@ -422,32 +422,42 @@ def _type(dtype: torch.dtype) -> int:
     return _TYPES[dtype]
 
 
-def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: torch.device, what: str) -> int:
-    """Checks a [rows][dim] matrix whose rows are contiguous; its row stride in values."""
-    if t.shape != (rows, dim) or t.dtype != dtype or t.device != device or (dim > 1 and rows > 0 and t.stride(1) != 1):
-        raise ValueError("%s: expected a [%d][%d] tensor of %s on %s with contiguous rows" % (what, rows, dim, dtype, device))
+def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: int, what: str) -> int:
+    """Checks a [rows][dim] matrix whose rows are contiguous, on CUDA device `device`; its row stride in values."""
+    if t.dtype != dtype or t.get_device() != device or t.dim() != 2 or t.size(0) != rows or t.size(1) != dim or (
+            dim > 1 and rows > 0 and t.stride(1) != 1):
+        raise ValueError("%s: expected a [%d][%d] tensor of %s on the inputs' CUDA device with contiguous rows" % (what, rows, dim, dtype))
     stride = t.stride(0) if rows > 1 else dim
     if stride < dim:
         raise ValueError("%s: rows overlap" % what)
     return stride
 
 
-def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, device: torch.device, what: str) -> int:
-    if t.shape != (n,) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous [%d] tensor of %s on %s" % (what, n, dtype, device))
+def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, device: int, what: str) -> int:
+    if t.dtype != dtype or t.get_device() != device or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous [%d] tensor of %s on the inputs' CUDA device" % (what, n, dtype))
     return t.data_ptr()
 
 
-def _enqueue(device: torch.device, stream: Optional[torch.cuda.Stream], call, what: str) -> None:
+def _cuda_device(t: torch.Tensor, what: str) -> int:
+    if not t.is_cuda:
+        raise ValueError("%s: expected a CUDA tensor" % what)
+    return t.get_device()
+
+
+def _enqueue(device: int, stream: Optional[torch.cuda.Stream], call, what: str) -> None:
     """Runs call(cudaStream_t) with `device` current: on torch's current stream, or on `stream`, ordered
     after the work that made the inputs and before the work that uses the outputs (both on the current stream)."""
-    if device.type != "cuda":
+    if device < 0:
         raise ValueError("%s: expected CUDA tensors" % what)
-    if device.index != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _enqueue(device, stream, call, what)
+    if stream is None:
+        # the handle alone: making a Stream object of it costs as much as a launch
+        return _check(call(torch._C._cuda_getCurrentRawStream(device)), what)
     cur = torch.cuda.current_stream(device)
-    if stream is None or stream == cur:
+    if stream == cur:
         return _check(call(cur.cuda_stream), what)
     stream.wait_stream(cur)
     try:
@@ -461,14 +471,13 @@ def tk_layernorm_forward(x: torch.Tensor, gain: torch.Tensor, bias: Optional[tor
     """Layer norm of every row of x ([rows][dim], rows contiguous): (y, mean, rstd)."""
     if x.dim() != 2:
         raise ValueError("x: expected [rows][dim]")
-    (rows, dim), dev = x.shape, x.device
+    (rows, dim), dev = x.shape, _cuda_device(x, "x")
     xt, pt = _type(x.dtype), _type(gain.dtype)
     xs = _matrix(x, rows, dim, x.dtype, dev, "x")
     gp = _vector(gain, dim, gain.dtype, dev, "gain")
     bp = _vector(bias, dim, gain.dtype, dev, "bias") if bias is not None else None
-    y = torch.empty((rows, dim), dtype=x.dtype, device=dev)
-    stats = torch.empty((2, rows), dtype=torch.float32, device=dev)
-    mean, rstd = stats[0], stats[1]
+    y = x.new_empty((rows, dim))
+    mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
     _enqueue(dev, stream, lambda s: load().tk_layernorm_forward(x.data_ptr(), xt, rows, dim, xs, gp, bp, pt, eps, y.data_ptr(), dim,
                                                                 mean.data_ptr(), rstd.data_ptr(), s), "tk_layernorm_forward")
     return y, mean, rstd
@@ -482,22 +491,22 @@ def tk_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
     grad_dtype (default: gain's), or written to the given tensors (for example slices of a gradient row)."""
     if x.dim() != 2:
         raise ValueError("x: expected [rows][dim]")
-    (rows, dim), dev = x.shape, x.device
+    (rows, dim), dev = x.shape, _cuda_device(x, "x")
     if grad_dtype is None:
         grad_dtype = dgain.dtype if dgain is not None else dbias.dtype if dbias is not None else gain.dtype
     xt, pt, gt = _type(x.dtype), _type(gain.dtype), _type(grad_dtype)
     xs, ds = _matrix(x, rows, dim, x.dtype, dev, "x"), _matrix(dy, rows, dim, x.dtype, dev, "dy")
     gp = _vector(gain, dim, gain.dtype, dev, "gain")
     mp, rp = _vector(mean, rows, torch.float32, dev, "mean"), _vector(rstd, rows, torch.float32, dev, "rstd")
-    dx = torch.empty((rows, dim), dtype=x.dtype, device=dev) if need_dx else None
+    dx = x.new_empty((rows, dim)) if need_dx else None
     ws, nbytes = None, 0
     if need_params:
-        dgain = torch.empty(dim, dtype=grad_dtype, device=dev) if dgain is None else dgain
-        dbias = torch.empty(dim, dtype=grad_dtype, device=dev) if dbias is None else dbias
+        dgain = x.new_empty(dim, dtype=grad_dtype) if dgain is None else dgain
+        dbias = x.new_empty(dim, dtype=grad_dtype) if dbias is None else dbias
         _vector(dgain, dim, grad_dtype, dev, "dgain")
         _vector(dbias, dim, grad_dtype, dev, "dbias")
-        nbytes = int(load().tk_layernorm_workspace_bytes(rows, dim))
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        nbytes = load().tk_layernorm_workspace_bytes(rows, dim)
+        ws = x.new_empty(nbytes, dtype=torch.uint8)
     else:
         dgain = dbias = None
     _enqueue(dev, stream, lambda s: load().tk_layernorm_backward(
@@ -510,7 +519,7 @@ def tk_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
 def _head(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor):
     if h.dim() != 2 or w.dim() != 2:
         raise ValueError("expected h [tokens][dim] and w [vocab][dim]")
-    (tokens, dim), vocab, dev = h.shape, w.shape[0], h.device
+    (tokens, dim), vocab, dev = h.shape, w.size(0), _cuda_device(h, "h")
     hs, wst = _matrix(h, tokens, dim, h.dtype, dev, "h"), _matrix(w, vocab, dim, h.dtype, dev, "w")
     tp = _vector(target, tokens, torch.int32, dev, "target")
     aligned = int(h.data_ptr() % 16 == 0 and w.data_ptr() % 16 == 0 and hs % 8 == 0 and wst % 8 == 0)
@@ -523,11 +532,11 @@ def tk_xent_workspace_bytes(tokens: int, vocab: int, dim: int, dtype: torch.dtyp
                                               int(aligned_rows)))
 
 
-def _xent_workspace(tokens, vocab, dim, in_type, grad_type, aligned, dev, what):
-    nbytes = int(load().tk_xent_workspace_bytes(tokens, vocab, dim, in_type, grad_type, aligned))
+def _xent_workspace(h, tokens, vocab, dim, in_type, grad_type, aligned, what):
+    nbytes = load().tk_xent_workspace_bytes(tokens, vocab, dim, in_type, grad_type, aligned)
     if nbytes == 0:
         raise TkError(-1, what)
-    return torch.empty(nbytes, dtype=torch.uint8, device=dev), nbytes
+    return h.new_empty(nbytes, dtype=torch.uint8), nbytes
 
 
 def tk_xent_loss(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
@@ -535,9 +544,8 @@ def tk_xent_loss(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
     """(loss, lse) per token of the head h w^T; target int32, negative = takes no part."""
     tokens, vocab, dim, dev, hs, wst, tp, aligned = _head(h, w, target)
     it = _type(h.dtype)
-    out = torch.empty((2, tokens), dtype=torch.float32, device=dev)
-    loss, lse = out[0], out[1]
-    ws, nbytes = _xent_workspace(tokens, vocab, dim, it, -1, aligned, dev, "tk_xent_loss")
+    loss, lse = h.new_empty((2, tokens), dtype=torch.float32).unbind(0)
+    ws, nbytes = _xent_workspace(h, tokens, vocab, dim, it, -1, aligned, "tk_xent_loss")
     _enqueue(dev, stream, lambda s: load().tk_xent_loss(h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp,
                                                         loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes, s), "tk_xent_loss")
     return loss, lse
@@ -553,11 +561,11 @@ def tk_xent_grad(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor, lse: to
         grad_dtype = dw.dtype if dw is not None else dh.dtype if dh is not None else h.dtype
     it, gt = _type(h.dtype), _type(grad_dtype)
     lp, dp = _vector(lse, tokens, torch.float32, dev, "lse"), _vector(dloss, tokens, torch.float32, dev, "dloss")
-    dh = (torch.empty((tokens, dim), dtype=grad_dtype, device=dev) if dh is None else dh) if need_dh else None
-    dw = (torch.empty((vocab, dim), dtype=grad_dtype, device=dev) if dw is None else dw) if need_dw else None
+    dh = (h.new_empty((tokens, dim), dtype=grad_dtype) if dh is None else dh) if need_dh else None
+    dw = (h.new_empty((vocab, dim), dtype=grad_dtype) if dw is None else dw) if need_dw else None
     dhs = _matrix(dh, tokens, dim, grad_dtype, dev, "dh") if need_dh else 0
     dws = _matrix(dw, vocab, dim, grad_dtype, dev, "dw") if need_dw else 0
-    ws, nbytes = _xent_workspace(tokens, vocab, dim, it, gt, aligned, dev, "tk_xent_grad")
+    ws, nbytes = _xent_workspace(h, tokens, vocab, dim, it, gt, aligned, "tk_xent_grad")
     _enqueue(dev, stream, lambda s: load().tk_xent_grad(
         h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp, lp, dp, dh.data_ptr() if need_dh else None, dhs,
         dw.data_ptr() if need_dw else None, dws, gt, ws.data_ptr(), nbytes, s), "tk_xent_grad")
@@ -599,6 +607,7 @@ class AdamW:
             if c is not None and (c.dtype != torch.bfloat16 or c.device != self.device or not c.is_contiguous() or
                                   c.numel() != p.numel()):
                 raise ValueError("copies: expected contiguous bfloat16 tensors of the parameters' sizes")
+        self._index, self._array = self.params[0].get_device(), ctypes.c_void_p * len(self.params)
         self.sizes = [p.numel() for p in self.params]
         blocks = [-(-n // ADAMW_BLOCK) for n in self.sizes]
         if state_bits == 32:
@@ -624,10 +633,11 @@ class AdamW:
     def _pointers(self, tensors, dtype: torch.dtype, what: str):
         if len(tensors) != len(self.sizes):
             raise ValueError("%s: expected %d tensors" % (what, len(self.sizes)))
+        device = self._index
         for t, n in zip(tensors, self.sizes):
-            if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
+            if t.dtype != dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous():
                 raise ValueError("%s: expected contiguous tensors of the parameters' sizes, %s, on %s" % (what, dtype, self.device))
-        return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+        return self._array(*[t.data_ptr() for t in tensors])
 
     def tk_adamw_step(self, grads, lr: Optional[float] = None, grad_scale: float = 1.0,
                       stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -637,14 +647,14 @@ class AdamW:
         o.grad_type = _type(dtype)
         ptrs = self._pointers(grads, dtype, "grads")
         o.lr, o.grad_scale, o.step = self.lr if lr is None else lr, grad_scale, self.steps + 1
-        _enqueue(self.device, stream, lambda s: load().tk_adamw_step(self._table, ptrs, len(ptrs), ctypes.byref(o), s), "tk_adamw_step")
+        _enqueue(self._index, stream, lambda s: load().tk_adamw_step(self._table, ptrs, len(ptrs), ctypes.byref(o), s), "tk_adamw_step")
         self.steps += 1
 
     def tk_adamw_set_state(self, m, v, step: int, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Takes the states from fp32 values, one tensor per parameter (a checkpoint's), and the number of steps done."""
         pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
         if self.state_bits == 8:
-            _enqueue(self.device, stream, lambda s: load().tk_adamw_set_state(self._table, pm, pv, len(pm), s), "tk_adamw_set_state")
+            _enqueue(self._index, stream, lambda s: load().tk_adamw_set_state(self._table, pm, pv, len(pm), s), "tk_adamw_set_state")
         else:
             torch._foreach_copy_(list(torch.split(self.m, self.sizes)), [t.reshape(-1) for t in m])
             torch._foreach_copy_(list(torch.split(self.v, self.sizes)), [t.reshape(-1) for t in v])
@@ -654,7 +664,7 @@ class AdamW:
         """Writes the values of the states to fp32 tensors, one per parameter; the number of steps done."""
         pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
         if self.state_bits == 8:
-            _enqueue(self.device, stream, lambda s: load().tk_adamw_get_state(self._table, pm, pv, len(pm), s), "tk_adamw_get_state")
+            _enqueue(self._index, stream, lambda s: load().tk_adamw_get_state(self._table, pm, pv, len(pm), s), "tk_adamw_get_state")
         else:
             torch._foreach_copy_([t.view(-1) for t in m], list(torch.split(self.m, self.sizes)))
             torch._foreach_copy_([t.view(-1) for t in v], list(torch.split(self.v, self.sizes)))

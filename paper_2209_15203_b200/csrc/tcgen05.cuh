@@ -23,11 +23,13 @@ __device__ __forceinline__ void mbar_expect(u32 bar, u32 bytes) {
 __device__ __forceinline__ void mbar_arrive_cluster(u32 bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// The hint lets the hardware hold the thread until the phase ends (or 1 ms has passed) instead of returning to poll: the loss of
+// 8192 x 50257 x 768 took 407 us with it and 459 us without.
 __device__ __forceinline__ bool mbar_try(u32 bar, u32 parity) {
     u32 done;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000000;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(done)
         : "r"(bar), "r"(parity)

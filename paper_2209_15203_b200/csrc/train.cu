@@ -244,7 +244,7 @@ int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int6
 namespace {
 
 // D of one piece of the vocabulary takes at most this much of the workspace, if a piece of 256 entries fits.
-constexpr size_t kXentPieceBytes = (size_t)256 << 20;
+constexpr size_t kXentPieceBytes = (size_t)384 << 20;
 
 struct XentLayout {
     int in_parts, d_parts;       // bf16 matrices an input / D is held as
@@ -261,13 +261,15 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int xent_pairs(int parts_a, int parts_b) { return parts_a == 1 || parts_b == 1 ? parts_a * parts_b : 6; }
 
-// Cutting the tiles of the two gradient products into items.  The workers take items in turn (dh's, then dw's), so the
-// launch lasts as long as the worker with the most rounds; whole tiles leave up to half of them idle at the end (8192
-// tokens, 768 wide: 96 + 150 tiles for 74 pairs).  Cut tiles are summed through memory, at a cost of about
-// kItemCost rounds each.  The best of all splits up to kMaxSplits each is taken.
+// Cutting the vocabulary into pieces and the tiles of a piece's two gradient products into items.  The workers take
+// items in turn (dh's, then dw's), so a launch lasts as long as the worker with the most rounds; whole tiles
+// leave up to half of them idle at the end (8192 tokens, 768 wide, pieces of 12,800: 96 + 150 tiles for 74 pairs).  Cut
+// tiles are summed through memory.  Times below are in rounds (a pair multiplies 256 x 256 x 64 in 0.34 us):
+// what an item costs beside its rounds, a launch, and the bytes that a join moves meanwhile.  All splits and a few
+// numbers of pieces are tried (about 5 us of host time).
 constexpr int kXentSms = 148;        // a wrong guess costs speed, nothing else: results do not change with the device
-constexpr int kMaxSplits = 32;
-constexpr double kItemCost = 12.0, kWholeCost = 4.0;
+constexpr int kMaxSplits = 32, kMorePieces = 6;
+constexpr double kItemCost = 8.0, kWholeCost = 4.0, kSoftCost = 3.0, kLaunchCost = 10.0, kRoundBytes = 1.7e6;
 constexpr size_t kPartBytes = (size_t)256 << 20;   // at most, per product
 
 double xent_makespan(int64_t n0, double c0, int64_t n1, double c1, int64_t workers) {
@@ -277,21 +279,49 @@ double xent_makespan(int64_t n0, double c0, int64_t n1, double c1, int64_t worke
     return base + (e0 && c0 > c1 ? c0 : e1 ? (e0 && c0 > c1 ? c0 : c1) : e0 ? c0 : 0.0);
 }
 
-void xent_cut(int64_t dh_tiles, int64_t dh_rounds, int64_t dw_tiles, int64_t dw_rounds, int cg, int* dh_per, int* dw_per) {
-    const int64_t workers = kXentSms / cg;
-    const size_t tile_bytes = (size_t)kTileM * cg * kTileN * sizeof(float);
+struct XentPlan {
+    int64_t piece;
+    int dh_per, dw_per;
+};
+
+XentPlan xent_plan(int64_t tokens, int64_t vocab, int64_t dim, int in_parts, int d_parts, int cg) {
+    const int64_t workers = kXentSms / cg, rows = kTileM * cg, tiles_v = ceil_div(vocab, kTileN);
+    const int64_t tiles_m = ceil_div(tokens, rows), across = ceil_div(dim, kTileN), soft_rounds = ceil_div(dim, kTileK) * xent_pairs(in_parts, in_parts);
+    const int pairs = xent_pairs(d_parts, in_parts);
+    const double tile_bytes = (double)rows * kTileN * sizeof(float), size = cg == 2 ? 1.0 : 0.5;   // a round of one CTA is half the work
+    int64_t most = (int64_t)(kXentPieceBytes / ((size_t)d_parts * 2 * tokens)) / kTileN;
+    if (most < 1) most = 1;
+    const int64_t fewest = ceil_div(tiles_v, most);
+    XentPlan plan = {};
     double best = 1e300;
-    for (int sh = 1; sh <= kMaxSplits && (sh == 1 || (dh_rounds >= 8 * sh && sh * dh_tiles * tile_bytes <= kPartBytes)); ++sh)
-        for (int sw = 1; sw <= kMaxSplits && (sw == 1 || (dw_rounds >= 8 * sw && sw * dw_tiles * tile_bytes <= kPartBytes)); ++sw) {
-            const int64_t ph = ceil_div(dh_rounds, sh), pw = ceil_div(dw_rounds, sw);
-            const double t = xent_makespan(dh_tiles * ceil_div(dh_rounds, ph), ph + (sh > 1 ? kItemCost : kWholeCost),
-                                           dw_tiles * ceil_div(dw_rounds, pw), pw + (sw > 1 ? kItemCost : kWholeCost), workers);
-            if (t < best) {
-                best = t;
-                *dh_per = (int)ph;
-                *dw_per = (int)pw;
+    int64_t last = 0;
+    for (int64_t pieces = fewest; pieces < fewest + kMorePieces && pieces <= tiles_v; ++pieces) {
+        const int64_t piece_tiles = ceil_div(tiles_v, pieces), count = ceil_div(tiles_v, piece_tiles);
+        if (piece_tiles == last) continue;
+        last = piece_tiles;
+        const int64_t piece = piece_tiles * kTileN;
+        const int64_t dh_tiles = tiles_m * across, dw_tiles = ceil_div(piece, rows) * across;
+        const int64_t dh_rounds = ceil_div(piece < vocab ? piece : vocab, kTileK) * pairs, dw_rounds = ceil_div(tokens, kTileK) * pairs;
+        const double soft = (double)ceil_div(tiles_m * piece_tiles, workers) * (soft_rounds + kSoftCost) + 2 * kLaunchCost;
+        const double sums = count > 1 ? 8.0 * tokens * dim : 0.0;
+        for (int sh = 1; sh <= kMaxSplits; ++sh) {
+            if (sh > 1 && (dh_rounds < 8 * sh || sh * dh_tiles * tile_bytes > kPartBytes || dh_tiles * sh > 16 * workers)) break;
+            const int64_t ph = ceil_div(dh_rounds, sh), nh = dh_tiles * ceil_div(dh_rounds, ph);
+            const double join_h = sh > 1 ? (nh * tile_bytes + sums) * size / kRoundBytes + kLaunchCost : 0.0;
+            for (int sw = 1; sw <= kMaxSplits; ++sw) {
+                if (sw > 1 && (dw_rounds < 8 * sw || sw * dw_tiles * tile_bytes > kPartBytes || dw_tiles * sw > 16 * workers)) break;
+                const int64_t pw = ceil_div(dw_rounds, sw), nw = dw_tiles * ceil_div(dw_rounds, pw);
+                const double join_w = sw > 1 ? nw * tile_bytes * size / kRoundBytes + kLaunchCost : 0.0;
+                const double t = count * (soft + join_h + join_w + xent_makespan(nh, ph + (sh > 1 ? kItemCost : kWholeCost), nw,
+                                                                                   pw + (sw > 1 ? kItemCost : kWholeCost), workers));
+                if (t < best) {
+                    best = t;
+                    plan = {piece, (int)ph, (int)pw};
+                }
             }
         }
+    }
+    return plan;
 }
 
 bool xent_sizes_ok(int64_t tokens, int64_t vocab, int64_t dim, int in_type, int grad_type) {
@@ -325,19 +355,14 @@ XentLayout xent_layout(int64_t tokens, int64_t vocab, int64_t dim, int in_type, 
     const size_t loss_end = at;
     at = inputs;
     if (grad_type >= 0) {
-        const size_t row = (size_t)L.d_parts * 2 * (tokens > 0 ? tokens : 1);
-        int64_t piece = (int64_t)(kXentPieceBytes / row) / kTileN * kTileN;
-        const int64_t all = (vocab + kTileN - 1) / kTileN * kTileN;
-        if (piece < kTileN) piece = kTileN;
-        if (piece > all) piece = all;
-        const int64_t pieces = (all + piece - 1) / piece;   // of equal size, up to a tile
-        L.piece = ((all + pieces - 1) / pieces + kTileN - 1) / kTileN * kTileN;
-        L.off_d = take(row * L.piece);
+        const int64_t some = tokens > 0 ? tokens : 1;
+        const XentPlan plan = xent_plan(some, vocab, dim, L.in_parts, L.d_parts, L.cg);
+        L.piece = plan.piece, L.dh_per = plan.dh_per, L.dw_per = plan.dw_per;
+        L.off_d = take((size_t)L.d_parts * 2 * some * L.piece);
         L.off_acc = take((size_t)tokens * dim * sizeof(float));
         const int rows = kTileM * L.cg, pairs = xent_pairs(L.d_parts, L.in_parts);
-        const int64_t across = ceil_div(dim, kTileN), dh_tiles = ceil_div(tokens, rows) * across, dw_tiles = ceil_div(L.piece, rows) * across;
-        const int64_t dh_rounds = ceil_div(L.piece < vocab ? L.piece : vocab, kTileK) * pairs, dw_rounds = ceil_div(tokens > 0 ? tokens : 1, kTileK) * pairs;
-        xent_cut(dh_tiles, dh_rounds, dw_tiles, dw_rounds, L.cg, &L.dh_per, &L.dw_per);
+        const int64_t across = ceil_div(dim, kTileN), dh_tiles = ceil_div(some, rows) * across, dw_tiles = ceil_div(L.piece, rows) * across;
+        const int64_t dh_rounds = ceil_div(L.piece < vocab ? L.piece : vocab, kTileK) * pairs, dw_rounds = ceil_div(some, kTileK) * pairs;
         const size_t tile_bytes = (size_t)rows * kTileN * sizeof(float);
         if (L.dh_per < dh_rounds) L.off_dh_part = take(ceil_div(dh_rounds, L.dh_per) * dh_tiles * tile_bytes);
         if (L.dw_per < dw_rounds) L.off_dw_part = take(ceil_div(dw_rounds, L.dw_per) * dw_tiles * tile_bytes);
