@@ -142,16 +142,6 @@ __device__ __forceinline__ void tmem_load32(u32 addr, float (&v)[32]) {
         : "r"(addr));
 }
 
-__device__ __forceinline__ void tmem_load16(u32 addr, float (&v)[16]) {
-    u32* r = (u32*)v;
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr));
-}
-
 // ---- matrix instructions ----
 // Shared-memory descriptor of an operand tile in the 128-byte swizzle: 1024-byte atoms of 8 rows x 128 bytes.
 // K-major: rows are M (or N), 64 values of K each; `stride` leads to the next 8 rows, `lead` is not used.

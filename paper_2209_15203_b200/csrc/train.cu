@@ -414,7 +414,7 @@ void set_segments(XentProblem& p, int parts_a, int parts_b) {
 template <int MODE, int CG, int PARTS>
 int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
     auto kernel = xent_kernel<MODE, CG, PARTS>;
-    constexpr int smem = XentShape<CG>::kSmem;
+    constexpr int smem = XentShape<CG, MODE>::kSmem;
     static bool ready[64];
     static int pairs[64];
     int dev = 0;

@@ -45,11 +45,12 @@ constexpr int kEpiCols = 128;       // columns an epilogue thread holds
 constexpr int kChunk = 8;
 constexpr int kBoxBytes = 64 * 64 * 2;                        // an MN-major box: 64 values x 64 of K
 constexpr int kABytes = kTileM * kTileK * 2;
-template <int CG> struct XentShape {
+template <int CG, int MODE> struct XentShape {
     static constexpr int kBRows = kTileN / CG;                // rows of the right operand this CTA holds
     static constexpr int kStageBytes = kABytes + kBRows * kTileK * 2;
-    static constexpr int kStages = CG == 1 ? 4 : 6;           // 192 KB either way
-    static constexpr int kStaging = 4096;                     // per epilogue warp
+    static constexpr int kStages = CG == 1 ? 4 : 6;           // 192 KB (kSoft with 5 stages and larger store buffers: 7 % slower)
+    // per epilogue warp: kSoft 32 x 64 values of D, swizzled; kGrad 32 x 32 values in rows of 33
+    static constexpr int kStaging = MODE == kXentSoft ? 4096 : 4224;
     static constexpr int kSmem = kStages * kStageBytes + kXentEpiWarps * kStaging + 512 + 1024;
 };
 
@@ -162,7 +163,7 @@ __device__ __forceinline__ u32 take_part(float& a, float& b, bool last) {
 
 template <int MODE, int CG, int PARTS>
 __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_constant__ XentArgs A) {
-    using S = XentShape<CG>;
+    using S = XentShape<CG, MODE>;
     extern __shared__ unsigned char raw[];
     const u32 base = (smem_addr(raw) + 1023u) & ~1023u;
     unsigned char* sm = raw + (base - smem_addr(raw));
@@ -306,28 +307,32 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
             }
             float v[kEpiCols];
             const int rounds = t.r1 - t.r0, chunk = P.chunk;
-            for (int r0 = 0; r0 < rounds; r0 += chunk, ++turn) {
-                const u32 slot = turn & 1;
-                if (!(ok = mbar_wait(done + 8 * slot, (turn >> 1) & 1))) break;
+            const u32 acc = tmem + half * kEpiCols + ((u32)(32 * quarter) << 16);
+            if ((ok = mbar_wait(done + 8 * (turn & 1), (turn >> 1) & 1))) {
                 tcgen05_fence_after();
-                const u32 acc = tmem + slot * kTileN + half * kEpiCols + ((u32)(32 * quarter) << 16);
-                if (r0 == 0) {
 #pragma unroll
-                    for (int c = 0; c < kEpiCols; c += 32) tmem_load32(acc + c, *(float(*)[32])(v + c));
+                for (int c = 0; c < kEpiCols; c += 32) tmem_load32(acc + (turn & 1) * kTileN + c, *(float(*)[32])(v + c));
+                tmem_load_wait();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(freed0 + 8 * (turn & 1));
+                ++turn;
+            }
+            for (int r0 = chunk; ok && r0 < rounds; r0 += chunk) {
+                if (!(ok = mbar_wait(done + 8 * (turn & 1), (turn >> 1) & 1))) break;
+                tcgen05_fence_after();
+#pragma unroll
+                for (int c = 0; c < kEpiCols; c += 32) {
+                    float x[32];
+                    tmem_load32(acc + (turn & 1) * kTileN + c, x);
                     tmem_load_wait();
-                } else {
 #pragma unroll
-                    for (int c = 0; c < kEpiCols; c += 16) {
-                        float x[16];
-                        tmem_load16(acc + c, x);
-                        tmem_load_wait();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[c + i] += x[i];
-                    }
+                    for (int i = 0; i < 32; ++i) v[c + i] += x[i];
                 }
                 tcgen05_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(freed0 + 8 * slot);
+                if (lane == 0) mbar_arrive_cluster(freed0 + 8 * (turn & 1));
+                ++turn;
             }
             if (!ok) {
                 if (lane == 0) atomicExch(A.status, 1);
@@ -428,14 +433,14 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                 for (int c = 0; c < kEpiCols; c += 32) {
                     __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) stage_ptr[lane * 32 + (i ^ lane)] = v[c + i];
+                    for (int i = 0; i < 32; ++i) stage_ptr[lane * 33 + i] = v[c + i];
                     __syncwarp();
                     if (c + lane < cols) {
                         float* to = sum + c + lane;
                         int64_t at = (int64_t)m0 * P.ld + n0 + c + lane;
 #pragma unroll 4
                         for (int r = 0; r < rows; ++r, to += pitch, at += P.ld) {
-                            float x = stage_ptr[r * 32 + (lane ^ r)];
+                            float x = stage_ptr[r * 33 + lane];
                             if (read) x += *to;
                             if (write) *to = x;
                             if (out) store_any(P.out, at, x, P.out_bf16);
