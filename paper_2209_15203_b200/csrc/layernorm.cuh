@@ -18,11 +18,35 @@
 namespace tk {
 
 constexpr int kNormThreads = 256;   // per CTA, unless a row needs a larger group
-constexpr int kNormFinishCols = 32, kNormFinishSlices = 8;
+constexpr int kNormFinishCols = 32, kNormFinishSlices = 32;
 
-template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Pack {
-    T v[VEC];
+// VEC values of a row as they lie in memory: one 16-byte load (a struct of bf16 values would be loaded one by one), or one value
+template <typename T, int VEC> struct Pack;
+template <> struct Pack<bf16, 8> {
+    uint4 w;
+    __device__ __forceinline__ void load(const bf16* p) { w = *(const uint4*)p; }
+    __device__ __forceinline__ float get(int i) const {
+        const u32 v = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+        return __uint_as_float(i & 1 ? v & 0xffff0000u : v << 16);
+    }
+    static __device__ __forceinline__ void store(bf16* p, const float (&v)[8]) {
+        __nv_bfloat162 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *(uint4*)p = make_uint4(*(u32*)&q[0], *(u32*)&q[1], *(u32*)&q[2], *(u32*)&q[3]);
+    }
+};
+template <> struct Pack<float, 4> {
+    float4 w;
+    __device__ __forceinline__ void load(const float* p) { w = *(const float4*)p; }
+    __device__ __forceinline__ float get(int i) const { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+    static __device__ __forceinline__ void store(float* p, const float (&v)[4]) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <typename T> struct Pack<T, 1> {
+    T w;
+    __device__ __forceinline__ void load(const T* p) { w = *p; }
+    __device__ __forceinline__ float get(int) const { return to_float(w); }
+    static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { *p = from_float<T>(v[0]); }
 };
 
 struct NormArgs {
@@ -43,43 +67,71 @@ struct NormArgs {
 // VEC parameters from column c as fp32
 template <int VEC>
 __device__ __forceinline__ void load_params(const void* p, int c, bool is_bf16, float (&out)[VEC]) {
-    if (VEC == 1) {
+    if constexpr (VEC == 1) {
         out[0] = load_any(p, c, is_bf16);
     } else if (is_bf16) {
-        constexpr int W = VEC < 8 ? VEC : 8;
+        if constexpr (VEC == 8) {
+            Pack<bf16, 8> q;
+            q.load((const bf16*)p + c);
 #pragma unroll
-        for (int i = 0; i < VEC; i += W) {
-            Pack<bf16, W> q = *(const Pack<bf16, W>*)((const bf16*)p + c + i);
-#pragma unroll
-            for (int j = 0; j < W; ++j) out[i + j] = to_float(q.v[j]);
+            for (int i = 0; i < 8; ++i) out[i] = q.get(i);
+        } else {
+            const uint2 q = *(const uint2*)((const bf16*)p + c);
+            out[0] = __uint_as_float(q.x << 16);
+            out[1] = __uint_as_float(q.x & 0xffff0000u);
+            out[2] = __uint_as_float(q.y << 16);
+            out[3] = __uint_as_float(q.y & 0xffff0000u);
         }
     } else {
-        constexpr int W = VEC < 4 ? VEC : 4;
 #pragma unroll
-        for (int i = 0; i < VEC; i += W) {
-            Pack<float, W> q = *(const Pack<float, W>*)((const float*)p + c + i);
-#pragma unroll
-            for (int j = 0; j < W; ++j) out[i + j] = q.v[j];
+        for (int i = 0; i < VEC; i += 4) {
+            const float4 q = *(const float4*)((const float*)p + c + i);
+            out[i] = q.x;
+            out[i + 1] = q.y;
+            out[i + 2] = q.z;
+            out[i + 3] = q.w;
         }
     }
 }
 
-// Sums of a and b over a group of G threads, in every thread.  red: one float2 per warp of the CTA and
-// buffer; consecutive calls alternate buffers (one barrier then separates reuse of a buffer).
+// Sums over a group of G threads, in every thread.  red: one float2 per warp of the CTA and buffer; consecutive
+// calls alternate buffers (one barrier then separates reuse of a buffer).
+__device__ __forceinline__ void group_barrier(int group, int threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(threads) : "memory");
+}
 template <int G>
-__device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int& buffer) {
+__device__ __forceinline__ float group_sum(float a, float2* red, int& buffer) {
     a = warp_sum(a);
-    b = warp_sum(b);
-    if (G == 32) return make_float2(a, b);
-    const int warp = threadIdx.x >> 5, first = (threadIdx.x / G) * (G / 32);
+    if (G == 32) return a;
     float2* r = red + buffer * 32;
     buffer ^= 1;
-    if ((threadIdx.x & 31) == 0) r[warp] = make_float2(a, b);
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)(threadIdx.x / G)), "n"(G) : "memory");
+    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5].x = a;
+    group_barrier(threadIdx.x / G, G);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < G / 32; ++i) s += r[threadIdx.x / G * (G / 32) + i].x;
+    return s;
+}
+// Two sums at once: the halves of a warp first exchange, then each half adds up one of the two (6 instead of 10 shuffles).
+template <int G>
+__device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int& buffer) {
+    const bool upper = threadIdx.x & 16;
+    float mine = upper ? b : a;
+    mine += __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (G == 32) {
+        const float other = __shfl_xor_sync(0xffffffffu, mine, 16);
+        return upper ? make_float2(other, mine) : make_float2(mine, other);
+    }
+    float2* r = red + buffer * 32;
+    buffer ^= 1;
+    if ((threadIdx.x & 15) == 0) ((float*)&r[threadIdx.x >> 5])[upper] = mine;
+    group_barrier(threadIdx.x / G, G);
     float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < G / 32; ++i) {
-        float2 v = r[first + i];
+        const float2 v = r[threadIdx.x / G * (G / 32) + i];
         s.x += v.x;
         s.y += v.y;
     }
@@ -88,26 +140,32 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int&
 
 // A group of G threads per row; thread t holds vectors t, t + G, ... (NV of them, VEC values each).
 template <typename T, int VEC, int NV, int G>
-__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads) norm_forward_kernel(const __grid_constant__ NormArgs A) {
+__device__ __forceinline__ void load_row(const T* x, int dim, Pack<T, VEC> (&q)[NV]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * G + (int)threadIdx.x % G) * VEC;
+        if (c < dim) q[j].load(x + c);
+    }
+}
+
+template <typename T, int VEC, int NV, int G>
+__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 3)
+    norm_forward_kernel(const __grid_constant__ NormArgs A) {
     __shared__ float2 red[64];
     const int t = threadIdx.x % G, groups = blockDim.x / G;
     const float inv = 1.0f / (float)A.dim;
     int buffer = 0;
     for (int64_t row = (int64_t)blockIdx.x * groups + threadIdx.x / G; row < A.rows; row += (int64_t)gridDim.x * groups) {
-        const T* x = (const T*)A.x + row * A.x_stride;
-        T* y = (T*)A.out + row * A.out_stride;
-        float v[NV][VEC], sum = 0.0f;
+        Pack<T, VEC> q[NV];
+        load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, q);
+        float v[NV][VEC], sum = 0.0f, sq = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int c = (j * G + t) * VEC;
-            if (c < A.dim) {
-                Pack<T, VEC> q = *(const Pack<T, VEC>*)(x + c);
+        for (int j = 0; j < NV; ++j)
+            if ((j * G + t) * VEC < A.dim) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sum += v[j][i] = to_float(q.v[i]);
+                for (int i = 0; i < VEC; ++i) sum += v[j][i] = q[j].get(i);
             }
-        }
-        const float mean = group_sum2<G>(sum, 0.0f, red, buffer).x * inv;
-        float sq = 0.0f;
+        const float mean = group_sum<G>(sum, red, buffer) * inv;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if ((j * G + t) * VEC < A.dim) {
@@ -117,32 +175,31 @@ __global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads) norm_forw
                     sq += v[j][i] * v[j][i];
                 }
             }
-        const float rstd = 1.0f / sqrtf(group_sum2<G>(sq, 0.0f, red, buffer).x * inv + A.eps);
+        const float rstd = 1.0f / sqrtf(group_sum<G>(sq, red, buffer) * inv + A.eps);
         if (t == 0 && A.mean) {
             A.mean[row] = mean;
             A.rstd[row] = rstd;
         }
+        T* y = (T*)A.out + row * A.out_stride;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + t) * VEC;
             if (c < A.dim) {
-                float gain[VEC], bias[VEC];
+                float gain[VEC], bias[VEC] = {};
                 load_params<VEC>(A.gain, c, A.param_bf16, gain);
                 if (A.bias) load_params<VEC>(A.bias, c, A.param_bf16, bias);
-                Pack<T, VEC> q;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float z = v[j][i] * rstd;
-                    q.v[i] = from_float<T>(A.bias ? z * gain[i] + bias[i] : z * gain[i]);
-                }
-                *(Pack<T, VEC>*)(y + c) = q;
+                for (int i = 0; i < VEC; ++i) v[j][i] = fmaf(v[j][i] * rstd, gain[i], bias[i]);
+                Pack<T, VEC>::store(y + c, v[j]);
             }
         }
     }
 }
 
+// The next row's x and dy are on their way while this row's sums go round the group.
 template <typename T, int VEC, int NV, int G>
-__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads) norm_backward_kernel(const __grid_constant__ NormArgs A) {
+__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 2)
+    norm_backward_kernel(const __grid_constant__ NormArgs A) {
     __shared__ float2 red[64];
     extern __shared__ float sums[];   // [2][dim] when several groups share the CTA
     const int t = threadIdx.x % G, groups = blockDim.x / G, group = threadIdx.x / G;
@@ -153,43 +210,55 @@ __global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads) norm_back
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dgain[j][i] = dbias[j][i] = 0.0f;
-    for (int64_t row = (int64_t)blockIdx.x * groups + group; row < A.rows; row += (int64_t)gridDim.x * groups) {
-        const T* x = (const T*)A.x + row * A.x_stride;
-        const T* dy = (const T*)A.dy + row * A.dy_stride;
-        const float mean = A.mean[row], rstd = A.rstd[row];
+    int64_t row = (int64_t)blockIdx.x * groups + group;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    Pack<T, VEC> x[NV], d[NV];
+    float mean = 0.0f, rstd = 0.0f;
+    if (row < A.rows) {
+        load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, x);
+        load_row<T, VEC, NV, G>((const T*)A.dy + row * A.dy_stride, A.dim, d);
+        mean = A.mean[row];
+        rstd = A.rstd[row];
+    }
+    while (row < A.rows) {
         float z[NV][VEC], u[NV][VEC], s1 = 0.0f, s2 = 0.0f;
+        const float r = rstd;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + t) * VEC;
             if (c < A.dim) {
-                Pack<T, VEC> qx = *(const Pack<T, VEC>*)(x + c);
-                Pack<T, VEC> qd = *(const Pack<T, VEC>*)(dy + c);
                 float gain[VEC];
                 load_params<VEC>(A.gain, c, A.param_bf16, gain);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    float d = to_float(qd.v[i]);
-                    z[j][i] = (to_float(qx.v[i]) - mean) * rstd;
-                    dgain[j][i] += d * z[j][i];
-                    dbias[j][i] += d;
-                    u[j][i] = d * gain[i];
+                    const float dy = d[j].get(i);
+                    z[j][i] = (x[j].get(i) - mean) * r;
+                    dgain[j][i] += dy * z[j][i];
+                    dbias[j][i] += dy;
+                    u[j][i] = dy * gain[i];
                     s1 += u[j][i];
                     s2 += u[j][i] * z[j][i];
                 }
             }
         }
+        T* dx = (T*)A.out + row * A.out_stride;
+        row += step;
+        if (row < A.rows) {
+            load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, x);
+            load_row<T, VEC, NV, G>((const T*)A.dy + row * A.dy_stride, A.dim, d);
+            mean = A.mean[row];
+            rstd = A.rstd[row];
+        }
         if (A.out) {
             const float2 s = group_sum2<G>(s1, s2, red, buffer);
-            const float a = s.x * inv, b = s.y * inv;
-            T* dx = (T*)A.out + row * A.out_stride;
+            const float a = s.x * inv * r, b = s.y * inv * r;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int c = (j * G + t) * VEC;
                 if (c < A.dim) {
-                    Pack<T, VEC> q;
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) q.v[i] = from_float<T>((u[j][i] - a - z[j][i] * b) * rstd);
-                    *(Pack<T, VEC>*)(dx + c) = q;
+                    for (int i = 0; i < VEC; ++i) u[j][i] = fmaf(-z[j][i], b, fmaf(u[j][i], r, -a));
+                    Pack<T, VEC>::store(dx + c, u[j]);
                 }
             }
         }
@@ -232,12 +301,12 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const __grid_constant__
         if (!backward) {
             float sum = 0.0f, sq = 0.0f;
             for (int c = threadIdx.x; c < A.dim; c += 1024) sum += to_float(x[c]);
-            const float mean = group_sum2<1024>(sum, 0.0f, red, buffer).x * inv;
+            const float mean = group_sum<1024>(sum, red, buffer) * inv;
             for (int c = threadIdx.x; c < A.dim; c += 1024) {
                 float d = to_float(x[c]) - mean;
                 sq += d * d;
             }
-            const float rstd = 1.0f / sqrtf(group_sum2<1024>(sq, 0.0f, red, buffer).x * inv + A.eps);
+            const float rstd = 1.0f / sqrtf(group_sum<1024>(sq, red, buffer) * inv + A.eps);
             if (threadIdx.x == 0 && A.mean) {
                 A.mean[row] = mean;
                 A.rstd[row] = rstd;
@@ -287,9 +356,18 @@ __global__ void __launch_bounds__(kNormFinishCols* kNormFinishSlices)
     __shared__ float part[kNormFinishSlices][kNormFinishCols];
     const int lane = threadIdx.x % kNormFinishCols, slice = threadIdx.x / kNormFinishCols;
     const int64_t c = (int64_t)blockIdx.x * kNormFinishCols + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // launched while the kernel before may still run
     float s = 0.0f;
-    if (c < 2 * (int64_t)dim)
-        for (int i = slice; i < parts; i += kNormFinishSlices) s += partial[(int64_t)i * 2 * dim + c];
+    if (c < 2 * (int64_t)dim) {
+        const float* at = partial + (int64_t)slice * 2 * dim + c;
+        const int64_t step = (int64_t)kNormFinishSlices * 2 * dim;
+        for (int i = slice; i < parts; i += 4 * kNormFinishSlices, at += 4 * step) {
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = i + j * kNormFinishSlices < parts ? at[j * step] : 0.0f;
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+    }
     part[slice][lane] = s;
     __syncthreads();
     if (slice == 0 && c < 2 * (int64_t)dim) {

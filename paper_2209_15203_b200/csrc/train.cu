@@ -24,6 +24,25 @@ int launch_error() {
     return TK_OK;
 }
 
+// Launches a kernel that begins with griddepcontrol.wait: its launch overlaps the end of the kernel before it.
+template <typename... KArgs, typename... Args>
+int launch_after(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...) != cudaSuccess) {
+        cudaGetLastError();
+        return TK_ERR_CUDA;
+    }
+    return TK_OK;
+}
+
 // Raised by a kernel whose bounded wait ran out; zero when the library is loaded.
 __device__ int g_status;
 
@@ -75,55 +94,53 @@ struct NormShape {
     int vec, nv, group;   // values per load, loads per thread, threads per row; group 0: the wide kernels
 };
 
-// The smallest group whose threads hold a row in at most 4 loads of 16 bytes each (or 8 single values).
-NormShape norm_shape(int dim, int type, bool wide_loads) {
+// Most loads per thread and row, and threads per row, of the forms that are built.  A forward thread holds up to 32 values of a row; a
+// backward thread 16, beside two sums for each and the next row's, in 128 registers.
+constexpr int norm_most(bool backward, int vec) { return vec == 1 ? 16 : (vec == 8 && backward ? 2 : 4); }
+constexpr int norm_unit(int most) { return most >= 4 ? most / 4 : 1; }
+constexpr int norm_widest(bool backward) { return backward ? 512 : 1024; }
+
+// The smallest group whose threads hold a row
+NormShape norm_shape(int dim, int type, bool wide_loads, bool backward) {
     const int vec = wide_loads ? (type == TK_BF16 ? 8 : 4) : 1;
-    const int vectors = (dim + vec - 1) / vec;
-    const int most = wide_loads ? 4 : 8;
-    for (int group : {32, 128, 512, 1024})
+    const int vectors = (dim + vec - 1) / vec, most = norm_most(backward, vec), unit = norm_unit(most);
+    for (int group = 32; group <= norm_widest(backward); group *= 2)
         if (vectors <= group * most) {
-            int nv = 1;
-            while (group * nv < vectors) nv *= 2;
-            return {vec, nv, group};
+            const int nv = ((vectors + group - 1) / group + unit - 1) / unit * unit;
+            return {vec, group > 32 && nv <= most / 2 ? most / 2 + unit : nv, group};
         }
     return {vec, 0, 0};
 }
 
-template <typename T, int VEC, int NV, int G>
-int launch_norm(const NormArgs& a, bool backward, int grid, cudaStream_t s) {
-    const int threads = G > kNormThreads ? G : kNormThreads;
-    if (backward) {
-        const size_t smem = threads / G > 1 ? (size_t)2 * a.dim * sizeof(float) : 0;
-        norm_backward_kernel<T, VEC, NV, G><<<grid, threads, smem, s>>>(a);
+template <bool BACKWARD, typename T, int VEC, int NV, int G>
+int launch_norm(int nv, const NormArgs& a, int grid, cudaStream_t s) {
+    constexpr int most = norm_most(BACKWARD, VEC), unit = norm_unit(most);
+    if constexpr (G > 32 && NV <= most / 2) {
+        return TK_ERR_INTERNAL;   // a smaller group holds such rows
     } else {
-        norm_forward_kernel<T, VEC, NV, G><<<grid, threads, 0, s>>>(a);
-    }
-    return launch_error();
-}
-template <typename T, int VEC, int G>
-int launch_norm(int nv, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
-    switch (nv) {
-        case 1: return launch_norm<T, VEC, 1, G>(a, backward, grid, s);
-        case 2: return launch_norm<T, VEC, 2, G>(a, backward, grid, s);
-        case 4: return launch_norm<T, VEC, 4, G>(a, backward, grid, s);
-        default:
-            if (VEC == 1) return launch_norm<T, VEC, VEC == 1 ? 8 : 4, G>(a, backward, grid, s);
+        if (nv < NV) {
+            if constexpr (NV > unit) return launch_norm<BACKWARD, T, VEC, NV - unit, G>(nv, a, grid, s);
             return TK_ERR_INTERNAL;
+        }
+        const int threads = G > kNormThreads ? G : kNormThreads;
+        if constexpr (BACKWARD)
+            norm_backward_kernel<T, VEC, NV, G><<<grid, threads, threads / G > 1 ? 2 * a.dim * sizeof(float) : 0, s>>>(a);
+        else
+            norm_forward_kernel<T, VEC, NV, G><<<grid, threads, 0, s>>>(a);
+        return launch_error();
     }
 }
-template <typename T, int VEC>
-int launch_norm(const NormShape& f, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
-    switch (f.group) {
-        case 32: return launch_norm<T, VEC, 32>(f.nv, a, backward, grid, s);
-        case 128: return launch_norm<T, VEC, 128>(f.nv, a, backward, grid, s);
-        case 512: return launch_norm<T, VEC, 512>(f.nv, a, backward, grid, s);
-        default: return launch_norm<T, VEC, 1024>(f.nv, a, backward, grid, s);
-    }
+template <bool BACKWARD, typename T, int VEC, int G = 32>
+int launch_norm(const NormShape& f, const NormArgs& a, int grid, cudaStream_t s) {
+    if (f.group == G) return launch_norm<BACKWARD, T, VEC, norm_most(BACKWARD, VEC), G>(f.nv, a, grid, s);
+    if constexpr (G < norm_widest(BACKWARD)) return launch_norm<BACKWARD, T, VEC, 2 * G>(f, a, grid, s);
+    return TK_ERR_INTERNAL;
 }
-int launch_norm(const NormShape& f, int type, const NormArgs& a, bool backward, int grid, cudaStream_t s) {
+template <bool BACKWARD>
+int launch_norm(const NormShape& f, int type, const NormArgs& a, int grid, cudaStream_t s) {
     if (type == TK_BF16)
-        return f.vec > 1 ? launch_norm<bf16, 8>(f, a, backward, grid, s) : launch_norm<bf16, 1>(f, a, backward, grid, s);
-    return f.vec > 1 ? launch_norm<float, 4>(f, a, backward, grid, s) : launch_norm<float, 1>(f, a, backward, grid, s);
+        return f.vec > 1 ? launch_norm<BACKWARD, bf16, 8>(f, a, grid, s) : launch_norm<BACKWARD, bf16, 1>(f, a, grid, s);
+    return f.vec > 1 ? launch_norm<BACKWARD, float, 4>(f, a, grid, s) : launch_norm<BACKWARD, float, 1>(f, a, grid, s);
 }
 
 bool norm_args_ok(int64_t rows, int64_t dim, int x_type, int param_type) {
@@ -155,7 +172,7 @@ int tk_layernorm_forward(const void* x, int x_type, int64_t rows, int64_t dim, i
     if (rc != TK_OK) return rc;
     const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(y, x_type, y_stride, dim) && aligned(gain, 16) &&
                       (!bias || aligned(bias, 16));
-    const NormShape f = norm_shape((int)dim, x_type, wide);
+    const NormShape f = norm_shape((int)dim, x_type, wide, false);
     NormArgs a = {};
     a.x = x, a.out = y, a.gain = gain, a.bias = bias, a.mean = mean, a.rstd = rstd;
     a.rows = rows, a.x_stride = x_stride, a.out_stride = y_stride;
@@ -171,7 +188,7 @@ int tk_layernorm_forward(const void* x, int x_type, int64_t rows, int64_t dim, i
     }
     const int per_cta = f.group > kNormThreads ? 1 : kNormThreads / f.group;
     const int64_t ctas = (rows + per_cta - 1) / per_cta, most = (int64_t)d->sms * 64;
-    return launch_norm(f, x_type, a, false, (int)(ctas < most ? ctas : most), s);
+    return launch_norm<false>(f, x_type, a, (int)(ctas < most ? ctas : most), s);
 }
 
 size_t tk_layernorm_workspace_bytes(int64_t rows, int64_t dim) {
@@ -201,7 +218,7 @@ int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int6
     if (rows > 0) {
         const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(dy, x_type, dy_stride, dim) &&
                           rows_wide(dx, x_type, dx_stride, dim) && aligned(gain, 16);
-        const NormShape f = norm_shape((int)dim, x_type, wide);
+        const NormShape f = norm_shape((int)dim, x_type, wide, true);
         NormArgs a = {};
         a.x = x, a.dy = dy, a.out = dx, a.gain = gain, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
         a.partial = params ? (float*)workspace : nullptr;
@@ -224,15 +241,14 @@ int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int6
             const int64_t ctas = (rows + per_cta - 1) / per_cta;
             const int64_t most = 2 * d->sms < kNormMaxParts ? 2 * d->sms : kNormMaxParts;
             parts = (int)(ctas < most ? ctas : most);
-            rc = launch_norm(f, x_type, a, true, parts, s);
+            rc = launch_norm<true>(f, x_type, a, parts, s);
         }
         if (rc != TK_OK) return rc;
     }
     if (params) {
         const unsigned grid = (unsigned)((2 * dim + kNormFinishCols - 1) / kNormFinishCols);
-        norm_finish_kernel<<<grid, kNormFinishCols * kNormFinishSlices, 0, s>>>((const float*)workspace, parts, (int)dim, dgain, dbias,
-                                                                                grad_type == TK_BF16);
-        rc = launch_error();
+        rc = launch_after(norm_finish_kernel, grid, kNormFinishCols * kNormFinishSlices, s, (const float*)workspace, parts, (int)dim,
+                          dgain, dbias, (int)(grad_type == TK_BF16));
     }
     return rc;
 }
