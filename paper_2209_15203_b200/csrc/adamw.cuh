@@ -26,9 +26,11 @@ namespace tk {
 
 constexpr int kAdamBlock = 256;     // values that share a scale
 constexpr int kAdamPerLane = kAdamBlock / 32;
-constexpr int kAdamThreads = 256;
+// Small CTAs that do one block per warp and leave: 124M values in 32 bits took 523 us so (6.6 TB/s), 549 us with 256 threads and two
+// blocks per warp, 554 us with four.
+constexpr int kAdamThreads = 128;
 constexpr int kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamChunk = 2 * kAdamWarps;   // blocks of 256 values per CTA
+constexpr int kAdamChunk = kAdamWarps;   // blocks of 256 values per CTA
 
 struct AdamEntry {
     char* p;
@@ -76,25 +78,73 @@ __device__ __forceinline__ int adam_find(const AdamGroup<CAP>& G, u32 chunk) {
 constexpr float kMagic = 8388608.0f;   // 2^23: adding it leaves an integer 0 .. 2^23 in the low mantissa bits
 constexpr float kLevelsM = 127.0f, kLevelsR = 255.0f;
 
-// byte j of a word as a float
-__device__ __forceinline__ float byte_float(u32 word, int j) {
-    return __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440 | j)) - kMagic;
+// Two fp32 values per instruction.  With 8-bit states the kernel is bound by the instructions it issues (90 per value without
+// this, 72 % of all issue slots), not by memory; each operation rounds as its scalar form does.  A packed product that is to be
+// rounded before something is added to it is added to by scalar instructions: the compiler contracts the packed forms.
+struct Pair {
+    u64 v;
+};
+__device__ __forceinline__ Pair pair(float a, float b) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
+__device__ __forceinline__ void split(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
 }
 
-// The code c of y = a / s: the number of thresholds k^2 + k + 1/2 (k = 0, 1, ..), the midpoints between k^2 and
-// (k+1)^2, that lie below y.  c is near round(sqrt(y - 1/4)); an approximate root gives it up to one, and
-// comparing with the two thresholds around it, which are exact in fp32, settles it.
-__device__ __forceinline__ float square_code(float y) {
-    float root;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(fmaxf(y - 0.25f, 0.0f)));
-    float c = (root + kMagic) - kMagic;
-    float t = fmaf(c, c, c) + 0.5f;
-    float down = fmaf(-2.0f, c, t);
-    if (y > t)
-        c += 1.0f;
-    else if (y <= down)
-        c -= 1.0f;
-    return fmaxf(c, 0.0f);
+// bytes j and j + 1 of a word in the low mantissa bits of 2^23
+__device__ __forceinline__ Pair byte_pair(u32 word, int j) {
+    return pair(__uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440 | j)),
+                __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440 | (j + 1))));
+}
+
+// Correctly rounded, with inputs below the smallest normal number taken as zero: a second moment that small has no part in a
+// step (its root is 1e-19 at most, beside eps).
+__device__ __forceinline__ float root_of(float v) {
+    float r;
+    asm("sqrt.rn.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float root_near(float v) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+__device__ __forceinline__ float reciprocal_near(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// The codes c of two y = a / s: the number of thresholds k^2 + k + 1/2 (k = 0, 1, ..), the midpoints between k^2 and (k+1)^2,
+// that lie below y; that is sqrt(y - 1/4) - 1/2 rounded up.  Rounding an approximate root of y - 0.3 to the nearest integer
+// gives c or c - 1 (the 0.05 lower the root by more than its error, 3e-5 at 255, and by less than one), and one comparison
+// with the threshold in question, exact in fp32 as y - 1/2 is, settles which.
+__device__ __forceinline__ void square_codes(Pair y, float& c0, float& c1) {
+    float l0, l1, t0, t1, h0, h1;
+    split(y + both(-0.3f), l0, l1);
+    const Pair c = pair(root_near(fmaxf(l0, 0.0f)), root_near(fmaxf(l1, 0.0f))) + both(kMagic) + both(-kMagic);
+    split(fma2(c, c, c), t0, t1);
+    split(y + both(-0.5f), h0, h1);
+    split(c, c0, c1);
+    if (h0 > t0) c0 += 1.0f;
+    if (h1 > t1) c1 += 1.0f;
 }
 
 // (scale, 1 / scale) of a block whose largest magnitude is `top`
@@ -108,20 +158,24 @@ __device__ __forceinline__ float block_max(float v) {   // v >= 0: its bits orde
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
 
+// The byte of m is its code with the sign, in two's complement; + 128 (an exclusive or of the top bit) makes it 1 .. 255
+constexpr float kMagicSigned = kMagic + 128.0f;
 __device__ __forceinline__ void decode_m(uint2 w, float s, float (&m)[kAdamPerLane]) {
+    w.x ^= 0x80808080u;
+    w.y ^= 0x80808080u;
 #pragma unroll
-    for (int k = 0; k < kAdamPerLane; ++k) {
-        u32 word = k < 4 ? w.x : w.y;
-        float c = byte_float(word & 0x7f7f7f7fu, k & 3);
-        u32 sign = (word << (24 - 8 * (k & 3))) & 0x80000000u;
-        m[k] = __uint_as_float(__float_as_uint(__fmul_rn(__fmul_rn(c, c), s)) | sign);
+    for (int k = 0; k < kAdamPerLane; k += 2) {
+        float a, b;
+        const Pair c = byte_pair(k < 4 ? w.x : w.y, k & 3) + both(-kMagicSigned);
+        split(c, a, b);
+        split(c * pair(fabsf(a), fabsf(b)) * both(s), m[k], m[k + 1]);
     }
 }
 __device__ __forceinline__ void decode_r(uint2 w, float s, float (&r)[kAdamPerLane]) {
 #pragma unroll
-    for (int k = 0; k < kAdamPerLane; ++k) {
-        float c = byte_float(k < 4 ? w.x : w.y, k & 3);
-        r[k] = __fmul_rn(__fmul_rn(c, c), s);
+    for (int k = 0; k < kAdamPerLane; k += 2) {
+        const Pair c = byte_pair(k < 4 ? w.x : w.y, k & 3) + both(-kMagic);
+        split(c * c * both(s), r[k], r[k + 1]);
     }
 }
 __device__ __forceinline__ u32 pack4(u32 a, u32 b, u32 c, u32 d) {
@@ -142,85 +196,119 @@ __device__ __forceinline__ void encode_block(const float (&m)[kAdamPerLane], con
     float2 sr = block_scale(block_max(tr), 1.0f / (kLevelsR * kLevelsR));
     u32 bm[kAdamPerLane], br[kAdamPerLane];
 #pragma unroll
-    for (int k = 0; k < kAdamPerLane; ++k) {
-        float c = square_code(__fmul_rn(fabsf(m[k]), sm.y));
-        bm[k] = (__float_as_uint(c + kMagic) & 0x7fu) | ((__float_as_uint(m[k]) >> 24) & 0x80u);
-        c = square_code(__fmul_rn(r[k], sr.y));
-        c = fmaxf(c, r[k] > 0.0f && sr.x > 0.0f ? 1.0f : 0.0f);
-        br[k] = __float_as_uint(c + kMagic) & 0xffu;
+    for (int k = 0; k < kAdamPerLane; k += 2) {
+        float c0, c1, y0, y1;
+        square_codes(pair(__fmul_rn(fabsf(m[k]), sm.y), __fmul_rn(fabsf(m[k + 1]), sm.y)), c0, c1);
+        bm[k] = __float_as_uint(copysignf(c0, m[k]) + kMagicSigned);
+        bm[k + 1] = __float_as_uint(copysignf(c1, m[k + 1]) + kMagicSigned);
+        // a positive r has code 1 at least: y is raised to 1 (in a block whose scale is zero the code does not matter)
+        y0 = __fmul_rn(r[k], sr.y);
+        y1 = __fmul_rn(r[k + 1], sr.y);
+        square_codes(pair(fmaxf(y0, __saturatef(r[k] * 1e38f)), fmaxf(y1, __saturatef(r[k + 1] * 1e38f))), c0, c1);
+        br[k] = __float_as_uint(c0 + kMagic);
+        br[k + 1] = __float_as_uint(c1 + kMagic);
     }
-    wm = make_uint2(pack4(bm[0], bm[1], bm[2], bm[3]), pack4(bm[4], bm[5], bm[6], bm[7]));
+    wm = make_uint2(pack4(bm[0], bm[1], bm[2], bm[3]) ^ 0x80808080u, pack4(bm[4], bm[5], bm[6], bm[7]) ^ 0x80808080u);
     wr = make_uint2(pack4(br[0], br[1], br[2], br[3]), pack4(br[4], br[5], br[6], br[7]));
     scales = make_float2(sm.x, sr.x);
 }
 
-template <typename P, typename G, int BITS, int CAP>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamGroup<CAP> A) {
-    const int at = adam_find(A, blockIdx.x);
-    const AdamEntry& e = A.e[at];
-    const AdamHyper& h = A.h;
-    const int lane = threadIdx.x & 31;
-    const int64_t blocks = (e.n + kAdamBlock - 1) / kAdamBlock;
-    const int64_t b0 = (int64_t)(blockIdx.x - e.first) * kAdamChunk + (threadIdx.x >> 5);
-    for (int64_t b = b0; b < b0 + kAdamChunk && b < blocks; b += kAdamWarps) {
-        const int64_t base = b * kAdamBlock + lane;
-        const int left = (int)min((int64_t)kAdamBlock, e.n - b * kAdamBlock) - lane;   // value k is there if 32 k < left
-        P* pp = (P*)e.p + base;
-        const G* gp = (const G*)e.g + base;
-        float p[kAdamPerLane], g[kAdamPerLane], m[kAdamPerLane], v[kAdamPerLane];
-        uint2 wm, wr;
-        float2 sc;
-        if (BITS == 8) {
-            wm = *(const uint2*)(e.m + b * kAdamBlock + lane * kAdamPerLane);
-            wr = *(const uint2*)(e.v + b * kAdamBlock + lane * kAdamPerLane);
-            sc = e.scales[b];
-        }
+// One block of 256 values by one warp; WHOLE: all 256 are there.
+template <typename P, typename G, int BITS, bool WHOLE>
+__device__ __forceinline__ void adamw_block(const AdamEntry& e, const AdamHyper& h, bool scaled, int64_t b, int lane) {
+    const int64_t base = b * kAdamBlock + lane;
+    const int left = WHOLE ? kAdamBlock : (int)(e.n - b * kAdamBlock) - lane;   // value k is there if 32 k < left
+    P* pp = (P*)e.p + base;
+    const G* gp = (const G*)e.g + base;
+    float* mp = (float*)e.m + base;
+    float* vp = (float*)e.v + base;
+    uint2* wmp = (uint2*)(e.m + b * kAdamBlock + lane * kAdamPerLane);
+    uint2* wrp = (uint2*)(e.v + b * kAdamBlock + lane * kAdamPerLane);
+    float p[kAdamPerLane], g[kAdamPerLane], m[kAdamPerLane], v[kAdamPerLane];
+    uint2 wm, wr;
+    float2 sc;
+    if (BITS == 8) {
+        wm = *wmp;
+        wr = *wrp;
+        sc = e.scales[b];
+    }
 #pragma unroll
-        for (int k = 0; k < kAdamPerLane; ++k) {
-            bool in = 32 * k < left;
-            p[k] = in ? to_float(pp[32 * k]) : 0.0f;
-            g[k] = in ? to_float(gp[32 * k]) : 0.0f;
-            if (BITS == 32) {
-                m[k] = in ? ((const float*)e.m)[base + 32 * k] : 0.0f;
-                v[k] = in ? ((const float*)e.v)[base + 32 * k] : 0.0f;
-            }
-        }
-        if (BITS == 8) {
-            decode_m(wm, sc.x, m);
-            decode_r(wr, sc.y, v);
-#pragma unroll
-            for (int k = 0; k < kAdamPerLane; ++k) v[k] = __fmul_rn(v[k], v[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kAdamPerLane; ++k) {
-            float gk = A.scaled ? __fmul_rn(g[k], h.gscale) : g[k];
-            m[k] = __fadd_rn(__fmul_rn(m[k], h.b1), __fmul_rn(gk, h.c1));
-            v[k] = __fadd_rn(__fmul_rn(v[k], h.b2), __fmul_rn(__fmul_rn(gk, h.c2), gk));
-            float r = __fsqrt_rn(v[k]);
-            float step = m[k] / (r * h.rbc2 + h.eps);
-            p[k] = (p[k] - e.decay * p[k]) - h.lr1 * step;
-            if (BITS == 32) {
-                if (32 * k < left) {
-                    ((float*)e.m)[base + 32 * k] = m[k];
-                    ((float*)e.v)[base + 32 * k] = v[k];
-                }
-            } else {
-                v[k] = r;
-            }
-            if (32 * k < left) {
-                P out = from_float<P>(p[k]);
-                pp[32 * k] = out;
-                if (e.copy16) e.copy16[base + 32 * k] = from_float<bf16>(to_float(out));
-            }
-        }
-        if (BITS == 8) {
-            // lanes past the end carry code 0 and gradient 0, so their m and r are 0 and stay 0
-            encode_block(m, v, wm, wr, sc);
-            *(uint2*)(e.m + b * kAdamBlock + lane * kAdamPerLane) = wm;
-            *(uint2*)(e.v + b * kAdamBlock + lane * kAdamPerLane) = wr;
-            if (lane == 0) e.scales[b] = sc;
+    for (int k = 0; k < kAdamPerLane; ++k) {
+        const bool in = WHOLE || 32 * k < left;
+        p[k] = in ? to_float(pp[32 * k]) : 0.0f;
+        g[k] = in ? to_float(gp[32 * k]) : 0.0f;
+        if (BITS == 32) {
+            m[k] = in ? mp[32 * k] : 0.0f;
+            v[k] = in ? vp[32 * k] : 0.0f;
         }
     }
+    if (BITS == 8) {
+        decode_m(wm, sc.x, m);
+        decode_r(wr, sc.y, v);
+    }
+#pragma unroll
+    for (int k = 0; k < kAdamPerLane; k += 2) {
+        Pair gk = pair(g[k], g[k + 1]), mk = pair(m[k], m[k + 1]), vk = pair(v[k], v[k + 1]), pk = pair(p[k], p[k + 1]);
+        if (BITS == 8) vk = vk * vk;
+        if (scaled) gk = gk * both(h.gscale);
+        float a0, a1, b0, b1;
+        split(mk * both(h.b1), a0, a1);
+        split(gk * both(h.c1), b0, b1);
+        m[k] = __fadd_rn(a0, b0);
+        m[k + 1] = __fadd_rn(a1, b1);
+        split(vk * both(h.b2), a0, a1);
+        split(gk * both(h.c2) * gk, b0, b1);
+        v[k] = __fadd_rn(a0, b0);
+        v[k + 1] = __fadd_rn(a1, b1);
+        mk = pair(m[k], m[k + 1]);
+        const float r0 = root_of(v[k]), r1 = root_of(v[k + 1]);
+        float d0, d1;
+        split(fma2(pair(r0, r1), both(h.rbc2), both(h.eps)), d0, d1);
+        // the approximate reciprocal is good to 1 unit in the last place, far inside the step's own rounding against p
+        const Pair step = mk * pair(reciprocal_near(d0), reciprocal_near(d1));
+        split(fma2(both(-h.lr1), step, fma2(both(-e.decay), pk, pk)), p[k], p[k + 1]);
+#pragma unroll
+        for (int i = k; i < k + 2; ++i)
+            if (WHOLE || 32 * i < left) {
+                if (BITS == 32) {
+                    mp[32 * i] = m[i];
+                    vp[32 * i] = v[i];
+                }
+                const P out = from_float<P>(p[i]);
+                pp[32 * i] = out;
+                p[i] = to_float(out);
+            }
+        if (BITS == 8) {
+            v[k] = r0;
+            v[k + 1] = r1;
+        }
+    }
+    if (e.copy16) {
+        bf16* to = e.copy16 + base;
+#pragma unroll
+        for (int k = 0; k < kAdamPerLane; ++k)
+            if (WHOLE || 32 * k < left) to[32 * k] = from_float<bf16>(p[k]);
+    }
+    if (BITS == 8) {
+        // lanes past the end carry code 0 and gradient 0, so their m and r are 0 and stay 0
+        encode_block(m, v, wm, wr, sc);
+        *wmp = wm;
+        *wrp = wr;
+        if (lane == 0) e.scales[b] = sc;
+    }
+}
+
+template <typename P, typename G, int BITS, int CAP>
+__global__ void __launch_bounds__(kAdamThreads, BITS == 8 ? 8 : 1) adamw_kernel(const __grid_constant__ AdamGroup<CAP> A) {
+    const AdamEntry e = A.e[adam_find(A, blockIdx.x)];
+    const int lane = threadIdx.x & 31;
+    const int64_t blocks = (e.n + kAdamBlock - 1) / kAdamBlock;
+    const int64_t b = (int64_t)(blockIdx.x - e.first) * kAdamChunk + (threadIdx.x >> 5);
+    if (b >= blocks) return;
+    if ((b + 1) * kAdamBlock <= e.n)
+        adamw_block<P, G, BITS, true>(e, A.h, A.scaled, b, lane);
+    else
+        adamw_block<P, G, BITS, false>(e, A.h, A.scaled, b, lane);
 }
 
 // 8-bit states from and to fp32 values (a checkpoint's): p holds m's values, g holds v's.
@@ -230,39 +318,38 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_state_kernel(const __grid_
     const AdamEntry& e = A.e[at];
     const int lane = threadIdx.x & 31;
     const int64_t blocks = (e.n + kAdamBlock - 1) / kAdamBlock;
-    const int64_t b0 = (int64_t)(blockIdx.x - e.first) * kAdamChunk + (threadIdx.x >> 5);
-    for (int64_t b = b0; b < b0 + kAdamChunk && b < blocks; b += kAdamWarps) {
-        const int64_t base = b * kAdamBlock + lane;
-        const int left = (int)min((int64_t)kAdamBlock, e.n - b * kAdamBlock) - lane;
-        float* mp = (float*)e.p + base;
-        float* vp = (float*)const_cast<char*>(e.g) + base;
-        uint2* wmp = (uint2*)(e.m + b * kAdamBlock + lane * kAdamPerLane);
-        uint2* wrp = (uint2*)(e.v + b * kAdamBlock + lane * kAdamPerLane);
-        float m[kAdamPerLane], r[kAdamPerLane];
-        if (LOAD) {
+    const int64_t b = (int64_t)(blockIdx.x - e.first) * kAdamChunk + (threadIdx.x >> 5);
+    if (b >= blocks) return;
+    const int64_t base = b * kAdamBlock + lane;
+    const int left = (int)min((int64_t)kAdamBlock, e.n - b * kAdamBlock) - lane;
+    float* mp = (float*)e.p + base;
+    float* vp = (float*)const_cast<char*>(e.g) + base;
+    uint2* wmp = (uint2*)(e.m + b * kAdamBlock + lane * kAdamPerLane);
+    uint2* wrp = (uint2*)(e.v + b * kAdamBlock + lane * kAdamPerLane);
+    float m[kAdamPerLane], r[kAdamPerLane];
+    if (LOAD) {
 #pragma unroll
-            for (int k = 0; k < kAdamPerLane; ++k) {
-                bool in = 32 * k < left;
-                m[k] = in ? mp[32 * k] : 0.0f;
-                r[k] = in ? __fsqrt_rn(vp[32 * k]) : 0.0f;
-            }
-            uint2 wm, wr;
-            float2 sc;
-            encode_block(m, r, wm, wr, sc);
-            *wmp = wm;
-            *wrp = wr;
-            if (lane == 0) e.scales[b] = sc;
-        } else {
-            float2 sc = e.scales[b];
-            decode_m(*wmp, sc.x, m);
-            decode_r(*wrp, sc.y, r);
-#pragma unroll
-            for (int k = 0; k < kAdamPerLane; ++k)
-                if (32 * k < left) {
-                    mp[32 * k] = m[k];
-                    vp[32 * k] = __fmul_rn(r[k], r[k]);
-                }
+        for (int k = 0; k < kAdamPerLane; ++k) {
+            bool in = 32 * k < left;
+            m[k] = in ? mp[32 * k] : 0.0f;
+            r[k] = in ? __fsqrt_rn(vp[32 * k]) : 0.0f;
         }
+        uint2 wm, wr;
+        float2 sc;
+        encode_block(m, r, wm, wr, sc);
+        *wmp = wm;
+        *wrp = wr;
+        if (lane == 0) e.scales[b] = sc;
+    } else {
+        float2 sc = e.scales[b];
+        decode_m(*wmp, sc.x, m);
+        decode_r(*wrp, sc.y, r);
+#pragma unroll
+        for (int k = 0; k < kAdamPerLane; ++k)
+            if (32 * k < left) {
+                mp[32 * k] = m[k];
+                vp[32 * k] = __fmul_rn(r[k], r[k]);
+            }
     }
 }
 
