@@ -78,34 +78,9 @@ __device__ __forceinline__ int adam_find(const AdamGroup<CAP>& G, u32 chunk) {
 constexpr float kMagic = 8388608.0f;   // 2^23: adding it leaves an integer 0 .. 2^23 in the low mantissa bits
 constexpr float kLevelsM = 127.0f, kLevelsR = 255.0f;
 
-// Two fp32 values per instruction.  With 8-bit states the kernel is bound by the instructions it issues (90 per value without
-// this, 72 % of all issue slots), not by memory; each operation rounds as its scalar form does.  A packed product that is to be
-// rounded before something is added to it is added to by scalar instructions: the compiler contracts the packed forms.
-struct Pair {
-    u64 v;
-};
-__device__ __forceinline__ Pair pair(float a, float b) {
-    Pair r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
-__device__ __forceinline__ void split(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
+// With 8-bit states the kernel is bound by the instructions it issues (90 per value with scalar arithmetic, 72 % of all issue
+// slots), not by memory: hence the packed operations.  A packed product that is to be rounded before something is added to it is
+// added to by scalar instructions: the compiler contracts the packed forms.
 
 // bytes j and j + 1 of a word in the low mantissa bits of 2^23
 __device__ __forceinline__ Pair byte_pair(u32 word, int j) {

@@ -25,6 +25,7 @@ template <typename T, int VEC> struct Pack;
 template <> struct Pack<bf16, 8> {
     uint4 w;
     __device__ __forceinline__ void load(const bf16* p) { w = *(const uint4*)p; }
+    __device__ __forceinline__ void clear() { w = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ float get(int i) const {
         const u32 v = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
         return __uint_as_float(i & 1 ? v & 0xffff0000u : v << 16);
@@ -39,12 +40,14 @@ template <> struct Pack<bf16, 8> {
 template <> struct Pack<float, 4> {
     float4 w;
     __device__ __forceinline__ void load(const float* p) { w = *(const float4*)p; }
+    __device__ __forceinline__ void clear() { w = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
     __device__ __forceinline__ float get(int i) const { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
     static __device__ __forceinline__ void store(float* p, const float (&v)[4]) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
 };
 template <typename T> struct Pack<T, 1> {
     T w;
     __device__ __forceinline__ void load(const T* p) { w = *p; }
+    __device__ __forceinline__ void clear() { w = from_float<T>(0.0f); }
     __device__ __forceinline__ float get(int) const { return to_float(w); }
     static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { *p = from_float<T>(v[0]); }
 };
@@ -61,7 +64,7 @@ struct NormArgs {
     int64_t rows, x_stride, dy_stride, out_stride;
     int dim;
     int param_bf16;
-    float eps;
+    float eps, inv;      // inv: 1 / dim
 };
 
 // VEC parameters from column c as fp32
@@ -138,129 +141,172 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int&
     return s;
 }
 
-// A group of G threads per row; thread t holds vectors t, t + G, ... (NV of them, VEC values each).
-template <typename T, int VEC, int NV, int G>
-__device__ __forceinline__ void load_row(const T* x, int dim, Pack<T, VEC> (&q)[NV]) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * G + (int)threadIdx.x % G) * VEC;
-        if (c < dim) q[j].load(x + c);
-    }
-}
-
-template <typename T, int VEC, int NV, int G>
-__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 3)
-    norm_forward_kernel(const __grid_constant__ NormArgs A) {
-    __shared__ float2 red[64];
-    const int t = threadIdx.x % G, groups = blockDim.x / G;
-    const float inv = 1.0f / (float)A.dim;
-    int buffer = 0;
-    for (int64_t row = (int64_t)blockIdx.x * groups + threadIdx.x / G; row < A.rows; row += (int64_t)gridDim.x * groups) {
-        Pack<T, VEC> q[NV];
-        load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, q);
-        float v[NV][VEC], sum = 0.0f, sq = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if ((j * G + t) * VEC < A.dim) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) sum += v[j][i] = q[j].get(i);
-            }
-        const float mean = group_sum<G>(sum, red, buffer) * inv;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if ((j * G + t) * VEC < A.dim) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    v[j][i] -= mean;
-                    sq += v[j][i] * v[j][i];
-                }
-            }
-        const float rstd = 1.0f / sqrtf(group_sum<G>(sq, red, buffer) * inv + A.eps);
-        if (t == 0 && A.mean) {
-            A.mean[row] = mean;
-            A.rstd[row] = rstd;
-        }
-        T* y = (T*)A.out + row * A.out_stride;
+// A group of G threads per row; thread t holds vectors t, t + G, ... (NV of them, VEC values each; a value that lies beyond the
+// row's end is zero).  Arithmetic is on pairs of values.
+template <typename T, int VEC, int NV, int G> struct RowPart {
+    static constexpr int kValues = VEC * NV, kPairs = kValues / 2;
+    static __device__ __forceinline__ int column(int j) { return (j * G + (int)threadIdx.x % G) * VEC; }
+    Pack<T, VEC> q[NV];
+    __device__ __forceinline__ void load(const T* row, int dim) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * G + t) * VEC;
-            if (c < A.dim) {
-                float gain[VEC], bias[VEC] = {};
-                load_params<VEC>(A.gain, c, A.param_bf16, gain);
-                if (A.bias) load_params<VEC>(A.bias, c, A.param_bf16, bias);
+            if (column(j) < dim)
+                q[j].load(row + column(j));
+            else
+                q[j].clear();
+        }
+    }
+    __device__ __forceinline__ Pair get(int p) const {
+        return pair(q[2 * p / VEC].get(2 * p % VEC), q[(2 * p + 1) / VEC].get((2 * p + 1) % VEC));
+    }
+    static __device__ __forceinline__ void store(T* row, int dim, const Pair (&v)[kPairs]) {
+        float x[kValues];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) v[j][i] = fmaf(v[j][i] * rstd, gain[i], bias[i]);
-                Pack<T, VEC>::store(y + c, v[j]);
+        for (int p = 0; p < kPairs; ++p) split(v[p], x[2 * p], x[2 * p + 1]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (column(j) < dim) Pack<T, VEC>::store(row + column(j), *(const float(*)[VEC])(x + j * VEC));
+    }
+    // `values` of the parameters for these columns (zeros where p is null)
+    static __device__ __forceinline__ void params(const void* p, bool is_bf16, int dim, Pair (&out)[kPairs]) {
+        float x[kValues] = {};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (p && column(j) < dim) load_params<VEC>(p, column(j), is_bf16, *(float(*)[VEC])(x + j * VEC));
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) out[i] = pair(x[2 * i], x[2 * i + 1]);
+    }
+};
+__device__ __forceinline__ float both_sum(Pair p) {
+    float a, b;
+    split(p, a, b);
+    return a + b;
+}
+constexpr __host__ __device__ int norm_rows(int vec) { return vec > 1 ? 2 : 1; }   // rows a group takes at once, forward
+
+// Two rows at a time: their sums go round the group together.  gain and bias stay in registers; the next rows are on their way
+// meanwhile.
+template <typename T, int VEC, int NV, int G>
+__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 2)
+    norm_forward_kernel(const __grid_constant__ NormArgs A) {
+    using Part = RowPart<T, VEC, NV, G>;
+    constexpr int R = norm_rows(VEC);
+    __shared__ float2 red[64];
+    const int t = threadIdx.x % G, groups = blockDim.x / G;
+    int buffer = 0;
+    const int64_t step = (int64_t)gridDim.x * groups * R;
+    int64_t row = ((int64_t)blockIdx.x * groups + threadIdx.x / G) * R;
+    Part x[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        if (row + k < A.rows) x[k].load((const T*)A.x + (row + k) * A.x_stride, A.dim);
+    Pair gain[Part::kPairs], bias[Part::kPairs];
+    Part::params(A.gain, A.param_bf16, A.dim, gain);
+    Part::params(A.bias, A.param_bf16, A.dim, bias);
+    for (; row < A.rows; row += step) {
+        Pair v[R][Part::kPairs];
+        float sum[2] = {0.0f, 0.0f}, mean[2], rstd[2];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            Pair s = both(0.0f);
+#pragma unroll
+            for (int i = 0; i < Part::kPairs; ++i) s = s + (v[k][i] = x[k].get(i));
+            sum[k] = both_sum(s);
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (row + step + k < A.rows) x[k].load((const T*)A.x + (row + step + k) * A.x_stride, A.dim);
+        float2 s = R == 2 ? group_sum2<G>(sum[0], sum[1], red, buffer) : make_float2(group_sum<G>(sum[0], red, buffer), 0.0f);
+        mean[0] = s.x * A.inv;
+        mean[1] = s.y * A.inv;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const Pair m = both(-mean[k]);
+            Pair sq = both(0.0f);
+#pragma unroll
+            for (int i = 0; i < Part::kPairs; ++i) {
+                v[k][i] = v[k][i] + m;
+                // what lies beyond the row's end has no part in the variance
+                if (VEC == 1) {
+                    float a, b;
+                    split(v[k][i], a, b);
+                    v[k][i] = pair(Part::column(2 * i) < A.dim ? a : 0.0f, Part::column(2 * i + 1) < A.dim ? b : 0.0f);
+                } else if (Part::column(2 * i / VEC) >= A.dim) {
+                    v[k][i] = both(0.0f);
+                }
+                sq = fma2(v[k][i], v[k][i], sq);
             }
+            sum[k] = both_sum(sq);
+        }
+        s = R == 2 ? group_sum2<G>(sum[0], sum[1], red, buffer) : make_float2(group_sum<G>(sum[0], red, buffer), 0.0f);
+        rstd[0] = rsqrtf(s.x * A.inv + A.eps);
+        rstd[1] = rsqrtf(s.y * A.inv + A.eps);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (row + k >= A.rows) break;
+            if (t == 0 && A.mean) {
+                A.mean[row + k] = mean[k];
+                A.rstd[row + k] = rstd[k];
+            }
+#pragma unroll
+            for (int i = 0; i < Part::kPairs; ++i) v[k][i] = fma2(v[k][i] * both(rstd[k]), gain[i], bias[i]);
+            Part::store((T*)A.out + (row + k) * A.out_stride, A.dim, v[k]);
         }
     }
 }
 
-// The next row's x and dy are on their way while this row's sums go round the group.
+// gain stays in registers, beside the two column sums of each value; the next row's x and dy are on their way while this row's
+// sums go round the group.
 template <typename T, int VEC, int NV, int G>
 __global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 2)
     norm_backward_kernel(const __grid_constant__ NormArgs A) {
+    using Part = RowPart<T, VEC, NV, G>;
     __shared__ float2 red[64];
     extern __shared__ float sums[];   // [2][dim] when several groups share the CTA
-    const int t = threadIdx.x % G, groups = blockDim.x / G, group = threadIdx.x / G;
-    const float inv = 1.0f / (float)A.dim;
+    const int groups = blockDim.x / G, group = threadIdx.x / G;
     int buffer = 0;
-    float dgain[NV][VEC], dbias[NV][VEC];
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) dgain[j][i] = dbias[j][i] = 0.0f;
     int64_t row = (int64_t)blockIdx.x * groups + group;
     const int64_t step = (int64_t)gridDim.x * groups;
-    Pack<T, VEC> x[NV], d[NV];
+    Part x, d;
     float mean = 0.0f, rstd = 0.0f;
     if (row < A.rows) {
-        load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, x);
-        load_row<T, VEC, NV, G>((const T*)A.dy + row * A.dy_stride, A.dim, d);
+        x.load((const T*)A.x + row * A.x_stride, A.dim);
+        d.load((const T*)A.dy + row * A.dy_stride, A.dim);
         mean = A.mean[row];
         rstd = A.rstd[row];
     }
+    Pair gain[Part::kPairs], dgain[Part::kPairs], dbias[Part::kPairs];
+    Part::params(A.gain, A.param_bf16, A.dim, gain);
+#pragma unroll
+    for (int i = 0; i < Part::kPairs; ++i) dgain[i] = dbias[i] = both(0.0f);
     while (row < A.rows) {
-        float z[NV][VEC], u[NV][VEC], s1 = 0.0f, s2 = 0.0f;
+        Pair z[Part::kPairs], u[Part::kPairs], s1 = both(0.0f), s2 = both(0.0f);
         const float r = rstd;
+        const Pair m = both(-mean), r2 = both(r);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int c = (j * G + t) * VEC;
-            if (c < A.dim) {
-                float gain[VEC];
-                load_params<VEC>(A.gain, c, A.param_bf16, gain);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float dy = d[j].get(i);
-                    z[j][i] = (x[j].get(i) - mean) * r;
-                    dgain[j][i] += dy * z[j][i];
-                    dbias[j][i] += dy;
-                    u[j][i] = dy * gain[i];
-                    s1 += u[j][i];
-                    s2 += u[j][i] * z[j][i];
-                }
-            }
+        for (int i = 0; i < Part::kPairs; ++i) {
+            const Pair dy = d.get(i);   // zero beyond the row's end: no part in any sum
+            z[i] = (x.get(i) + m) * r2;
+            dgain[i] = fma2(dy, z[i], dgain[i]);
+            dbias[i] = dbias[i] + dy;
+            u[i] = dy * gain[i];
+            s1 = s1 + u[i];
+            s2 = fma2(u[i], z[i], s2);
         }
         T* dx = (T*)A.out + row * A.out_stride;
         row += step;
         if (row < A.rows) {
-            load_row<T, VEC, NV, G>((const T*)A.x + row * A.x_stride, A.dim, x);
-            load_row<T, VEC, NV, G>((const T*)A.dy + row * A.dy_stride, A.dim, d);
+            x.load((const T*)A.x + row * A.x_stride, A.dim);
+            d.load((const T*)A.dy + row * A.dy_stride, A.dim);
             mean = A.mean[row];
             rstd = A.rstd[row];
         }
         if (A.out) {
-            const float2 s = group_sum2<G>(s1, s2, red, buffer);
-            const float a = s.x * inv * r, b = s.y * inv * r;
+            const float2 s = group_sum2<G>(both_sum(s1), both_sum(s2), red, buffer);
+            const Pair a = both(-s.x * A.inv * r), b = both(-s.y * A.inv * r);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int c = (j * G + t) * VEC;
-                if (c < A.dim) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) u[j][i] = fmaf(-z[j][i], b, fmaf(u[j][i], r, -a));
-                    Pack<T, VEC>::store(dx + c, u[j]);
-                }
-            }
+            for (int i = 0; i < Part::kPairs; ++i) u[i] = fma2(z[i], b, fma2(u[i], r2, a));
+            Part::store(dx, A.dim, u);
         }
     }
     if (!A.partial) return;
@@ -269,18 +315,20 @@ __global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNorm
         if (turn == group) {
             float* to = turn == groups - 1 ? mine : sums;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int c = (j * G + t) * VEC;
-                if (c < A.dim) {
+            for (int i = 0; i < Part::kPairs; ++i) {
+                float a[2], b[2];
+                split(dgain[i], a[0], a[1]);
+                split(dbias[i], b[0], b[1]);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        float a = dgain[j][i], b = dbias[j][i];
+                for (int k = 0; k < 2; ++k) {
+                    const int e = 2 * i + k, c = Part::column(e / VEC) + e % VEC;
+                    if (c < A.dim) {
                         if (turn > 0) {
-                            a += sums[c + i];
-                            b += sums[A.dim + c + i];
+                            a[k] += sums[c];
+                            b[k] += sums[A.dim + c];
                         }
-                        to[c + i] = a;
-                        to[A.dim + c + i] = b;
+                        to[c] = a[k];
+                        to[A.dim + c] = b[k];
                     }
                 }
             }
@@ -293,7 +341,7 @@ __global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNorm
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_wide_kernel(const __grid_constant__ NormArgs A, int backward) {
     __shared__ float2 red[64];
-    const float inv = 1.0f / (float)A.dim;
+    const float inv = A.inv;
     int buffer = 0;
     for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
         const T* x = (const T*)A.x + row * A.x_stride;
@@ -306,7 +354,7 @@ __global__ void __launch_bounds__(1024) norm_wide_kernel(const __grid_constant__
                 float d = to_float(x[c]) - mean;
                 sq += d * d;
             }
-            const float rstd = 1.0f / sqrtf(group_sum<1024>(sq, red, buffer) * inv + A.eps);
+            const float rstd = rsqrtf(group_sum<1024>(sq, red, buffer) * inv + A.eps);
             if (threadIdx.x == 0 && A.mean) {
                 A.mean[row] = mean;
                 A.rstd[row] = rstd;

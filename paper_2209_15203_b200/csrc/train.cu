@@ -94,17 +94,16 @@ struct NormShape {
     int vec, nv, group;   // values per load, loads per thread, threads per row; group 0: the wide kernels
 };
 
-// Most loads per thread and row, and threads per row, of the forms that are built.  A forward thread holds up to 32 values of a row; a
-// backward thread 16, beside two sums for each and the next row's, in 128 registers.
-constexpr int norm_most(bool backward, int vec) { return vec == 1 ? 16 : (vec == 8 && backward ? 2 : 4); }
-constexpr int norm_unit(int most) { return most >= 4 ? most / 4 : 1; }
-constexpr int norm_widest(bool backward) { return backward ? 512 : 1024; }
+// Values of a row per thread, and threads per row, of the forms that are built
+constexpr int norm_most(int vec) { return 16 / vec; }
+constexpr int norm_unit(int vec) { return vec == 8 ? 1 : norm_most(vec) / 4; }
+constexpr int kNormWidest = 1024;
 
 // The smallest group whose threads hold a row
-NormShape norm_shape(int dim, int type, bool wide_loads, bool backward) {
+NormShape norm_shape(int dim, int type, bool wide_loads) {
     const int vec = wide_loads ? (type == TK_BF16 ? 8 : 4) : 1;
-    const int vectors = (dim + vec - 1) / vec, most = norm_most(backward, vec), unit = norm_unit(most);
-    for (int group = 32; group <= norm_widest(backward); group *= 2)
+    const int vectors = (dim + vec - 1) / vec, most = norm_most(vec), unit = norm_unit(vec);
+    for (int group = 32; group <= kNormWidest; group *= 2)
         if (vectors <= group * most) {
             const int nv = ((vectors + group - 1) / group + unit - 1) / unit * unit;
             return {vec, group > 32 && nv <= most / 2 ? most / 2 + unit : nv, group};
@@ -114,7 +113,7 @@ NormShape norm_shape(int dim, int type, bool wide_loads, bool backward) {
 
 template <bool BACKWARD, typename T, int VEC, int NV, int G>
 int launch_norm(int nv, const NormArgs& a, int grid, cudaStream_t s) {
-    constexpr int most = norm_most(BACKWARD, VEC), unit = norm_unit(most);
+    constexpr int most = norm_most(VEC), unit = norm_unit(VEC);
     if constexpr (G > 32 && NV <= most / 2) {
         return TK_ERR_INTERNAL;   // a smaller group holds such rows
     } else {
@@ -122,9 +121,9 @@ int launch_norm(int nv, const NormArgs& a, int grid, cudaStream_t s) {
             if constexpr (NV > unit) return launch_norm<BACKWARD, T, VEC, NV - unit, G>(nv, a, grid, s);
             return TK_ERR_INTERNAL;
         }
-        const int threads = G > kNormThreads ? G : kNormThreads;
+        constexpr int threads = G > kNormThreads ? G : kNormThreads;
         if constexpr (BACKWARD)
-            norm_backward_kernel<T, VEC, NV, G><<<grid, threads, threads / G > 1 ? 2 * a.dim * sizeof(float) : 0, s>>>(a);
+            norm_backward_kernel<T, VEC, NV, G><<<grid, threads, threads > G ? 2 * a.dim * sizeof(float) : 0, s>>>(a);
         else
             norm_forward_kernel<T, VEC, NV, G><<<grid, threads, 0, s>>>(a);
         return launch_error();
@@ -132,8 +131,8 @@ int launch_norm(int nv, const NormArgs& a, int grid, cudaStream_t s) {
 }
 template <bool BACKWARD, typename T, int VEC, int G = 32>
 int launch_norm(const NormShape& f, const NormArgs& a, int grid, cudaStream_t s) {
-    if (f.group == G) return launch_norm<BACKWARD, T, VEC, norm_most(BACKWARD, VEC), G>(f.nv, a, grid, s);
-    if constexpr (G < norm_widest(BACKWARD)) return launch_norm<BACKWARD, T, VEC, 2 * G>(f, a, grid, s);
+    if (f.group == G) return launch_norm<BACKWARD, T, VEC, norm_most(VEC), G>(f.nv, a, grid, s);
+    if constexpr (G < kNormWidest) return launch_norm<BACKWARD, T, VEC, 2 * G>(f, a, grid, s);
     return TK_ERR_INTERNAL;
 }
 template <bool BACKWARD>
@@ -172,11 +171,11 @@ int tk_layernorm_forward(const void* x, int x_type, int64_t rows, int64_t dim, i
     if (rc != TK_OK) return rc;
     const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(y, x_type, y_stride, dim) && aligned(gain, 16) &&
                       (!bias || aligned(bias, 16));
-    const NormShape f = norm_shape((int)dim, x_type, wide, false);
+    const NormShape f = norm_shape((int)dim, x_type, wide);
     NormArgs a = {};
     a.x = x, a.out = y, a.gain = gain, a.bias = bias, a.mean = mean, a.rstd = rstd;
     a.rows = rows, a.x_stride = x_stride, a.out_stride = y_stride;
-    a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16, a.eps = eps;
+    a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16, a.eps = eps, a.inv = 1.0f / (float)dim;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     if (!f.group) {
         const int grid = (int)(rows < 4 * d->sms ? rows : 4 * d->sms);
@@ -187,7 +186,7 @@ int tk_layernorm_forward(const void* x, int x_type, int64_t rows, int64_t dim, i
         return launch_error();
     }
     const int per_cta = f.group > kNormThreads ? 1 : kNormThreads / f.group;
-    const int64_t ctas = (rows + per_cta - 1) / per_cta, most = (int64_t)d->sms * 64;
+    const int64_t per = (int64_t)per_cta * norm_rows(f.vec), ctas = (rows + per - 1) / per, most = 2 * (int64_t)d->sms;
     return launch_norm<false>(f, x_type, a, (int)(ctas < most ? ctas : most), s);
 }
 
@@ -218,12 +217,12 @@ int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int6
     if (rows > 0) {
         const bool wide = rows_wide(x, x_type, x_stride, dim) && rows_wide(dy, x_type, dy_stride, dim) &&
                           rows_wide(dx, x_type, dx_stride, dim) && aligned(gain, 16);
-        const NormShape f = norm_shape((int)dim, x_type, wide, true);
+        const NormShape f = norm_shape((int)dim, x_type, wide);
         NormArgs a = {};
         a.x = x, a.dy = dy, a.out = dx, a.gain = gain, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
         a.partial = params ? (float*)workspace : nullptr;
         a.rows = rows, a.x_stride = x_stride, a.dy_stride = dy_stride, a.out_stride = dx_stride;
-        a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16;
+        a.dim = (int)dim, a.param_bf16 = param_type == TK_BF16, a.inv = 1.0f / (float)dim;
         if (!f.group) {
             const int grid = (int)(rows < 4 * d->sms ? rows : 4 * d->sms);
             parts = (int)(rows < kNormWideParts ? rows : kNormWideParts);
