@@ -424,9 +424,12 @@ def _type(dtype: torch.dtype) -> int:
 
 def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: int, what: str) -> int:
     """Checks a [rows][dim] matrix whose rows are contiguous, on CUDA device `device`; its row stride in values."""
-    if t.dtype != dtype or t.get_device() != device or t.dim() != 2 or t.size(0) != rows or t.size(1) != dim or (
-            dim > 1 and rows > 0 and t.stride(1) != 1):
-        raise ValueError("%s: expected a [%d][%d] tensor of %s on the inputs' CUDA device with contiguous rows" % (what, rows, dim, dtype))
+    if t.shape != (rows, dim) or t.dtype != dtype or t.get_device() != device:
+        raise ValueError("%s: expected a [%d][%d] tensor of %s on the inputs' CUDA device" % (what, rows, dim, dtype))
+    if t.is_contiguous():
+        return dim
+    if dim > 1 and rows > 0 and t.stride(1) != 1:
+        raise ValueError("%s: expected contiguous rows" % what)
     stride = t.stride(0) if rows > 1 else dim
     if stride < dim:
         raise ValueError("%s: rows overlap" % what)
@@ -434,36 +437,31 @@ def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: in
 
 
 def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, device: int, what: str) -> int:
-    if t.dtype != dtype or t.get_device() != device or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous [%d] tensor of %s on the inputs' CUDA device" % (what, n, dtype))
     return t.data_ptr()
 
 
-def _cuda_device(t: torch.Tensor, what: str) -> int:
-    if not t.is_cuda:
-        raise ValueError("%s: expected a CUDA tensor" % what)
-    return t.get_device()
-
-
-def _enqueue(device: int, stream: Optional[torch.cuda.Stream], call, what: str) -> None:
-    """Runs call(cudaStream_t) with `device` current: on torch's current stream, or on `stream`, ordered
+def _enqueue(device: int, stream: Optional[torch.cuda.Stream], what: str, fn, *args) -> None:
+    """Calls fn(*args, cudaStream_t) with `device` current: on torch's current stream, or on `stream`, ordered
     after the work that made the inputs and before the work that uses the outputs (both on the current stream)."""
     if device < 0:
         raise ValueError("%s: expected CUDA tensors" % what)
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _enqueue(device, stream, call, what)
+            return _enqueue(device, stream, what, fn, *args)
     if stream is None:
         # the handle alone: making a Stream object of it costs as much as a launch
-        return _check(call(torch._C._cuda_getCurrentRawStream(device)), what)
-    cur = torch.cuda.current_stream(device)
-    if stream == cur:
-        return _check(call(cur.cuda_stream), what)
-    stream.wait_stream(cur)
-    try:
-        _check(call(stream.cuda_stream), what)
-    finally:
-        cur.wait_stream(stream)
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        cur = torch.cuda.current_stream(device)
+        if stream != cur:
+            stream.wait_stream(cur)
+        code = fn(*args, stream.cuda_stream)
+        if stream != cur:
+            cur.wait_stream(stream)
+    if code != 0:
+        raise TkError(code, what)
 
 
 def tk_layernorm_forward(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -471,15 +469,14 @@ def tk_layernorm_forward(x: torch.Tensor, gain: torch.Tensor, bias: Optional[tor
     """Layer norm of every row of x ([rows][dim], rows contiguous): (y, mean, rstd)."""
     if x.dim() != 2:
         raise ValueError("x: expected [rows][dim]")
-    (rows, dim), dev = x.shape, _cuda_device(x, "x")
-    xt, pt = _type(x.dtype), _type(gain.dtype)
-    xs = _matrix(x, rows, dim, x.dtype, dev, "x")
-    gp = _vector(gain, dim, gain.dtype, dev, "gain")
-    bp = _vector(bias, dim, gain.dtype, dev, "bias") if bias is not None else None
+    (rows, dim), dev, dtype, param = x.shape, x.get_device(), x.dtype, gain.dtype
+    xt, pt = _type(dtype), _type(param)
+    xs, gp = _matrix(x, rows, dim, dtype, dev, "x"), _vector(gain, dim, param, dev, "gain")
+    bp = _vector(bias, dim, param, dev, "bias") if bias is not None else None
     y = x.new_empty((rows, dim))
     mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
-    _enqueue(dev, stream, lambda s: load().tk_layernorm_forward(x.data_ptr(), xt, rows, dim, xs, gp, bp, pt, eps, y.data_ptr(), dim,
-                                                                mean.data_ptr(), rstd.data_ptr(), s), "tk_layernorm_forward")
+    _enqueue(dev, stream, "tk_layernorm_forward", load().tk_layernorm_forward, x.data_ptr(), xt, rows, dim, xs, gp, bp, pt, eps,
+             y.data_ptr(), dim, mean.data_ptr(), rstd.data_ptr())
     return y, mean, rstd
 
 
@@ -491,39 +488,45 @@ def tk_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
     grad_dtype (default: gain's), or written to the given tensors (for example slices of a gradient row)."""
     if x.dim() != 2:
         raise ValueError("x: expected [rows][dim]")
-    (rows, dim), dev = x.shape, _cuda_device(x, "x")
+    (rows, dim), dev, dtype, param = x.shape, x.get_device(), x.dtype, gain.dtype
     if grad_dtype is None:
-        grad_dtype = dgain.dtype if dgain is not None else dbias.dtype if dbias is not None else gain.dtype
-    xt, pt, gt = _type(x.dtype), _type(gain.dtype), _type(grad_dtype)
-    xs, ds = _matrix(x, rows, dim, x.dtype, dev, "x"), _matrix(dy, rows, dim, x.dtype, dev, "dy")
-    gp = _vector(gain, dim, gain.dtype, dev, "gain")
+        grad_dtype = dgain.dtype if dgain is not None else dbias.dtype if dbias is not None else param
+    xt, pt, gt = _type(dtype), _type(param), _type(grad_dtype)
+    xs, ds = _matrix(x, rows, dim, dtype, dev, "x"), _matrix(dy, rows, dim, dtype, dev, "dy")
+    gp = _vector(gain, dim, param, dev, "gain")
     mp, rp = _vector(mean, rows, torch.float32, dev, "mean"), _vector(rstd, rows, torch.float32, dev, "rstd")
-    dx = x.new_empty((rows, dim)) if need_dx else None
-    ws, nbytes = None, 0
+    lib = load()
+    dx, dxp = None, None
+    if need_dx:
+        dx = x.new_empty((rows, dim))
+        dxp = dx.data_ptr()
+    dgp = dbp = wsp = None
+    nbytes = 0
     if need_params:
+        if dgain is None and dbias is None:
+            dgain, dbias = x.new_empty((2, dim), dtype=grad_dtype).unbind(0)
         dgain = x.new_empty(dim, dtype=grad_dtype) if dgain is None else dgain
         dbias = x.new_empty(dim, dtype=grad_dtype) if dbias is None else dbias
-        _vector(dgain, dim, grad_dtype, dev, "dgain")
-        _vector(dbias, dim, grad_dtype, dev, "dbias")
-        nbytes = load().tk_layernorm_workspace_bytes(rows, dim)
+        dgp, dbp = _vector(dgain, dim, grad_dtype, dev, "dgain"), _vector(dbias, dim, grad_dtype, dev, "dbias")
+        nbytes = lib.tk_layernorm_workspace_bytes(rows, dim)
         ws = x.new_empty(nbytes, dtype=torch.uint8)
+        wsp = ws.data_ptr()
     else:
         dgain = dbias = None
-    _enqueue(dev, stream, lambda s: load().tk_layernorm_backward(
-        dy.data_ptr(), ds, x.data_ptr(), xs, xt, rows, dim, gp, pt, mp, rp, dx.data_ptr() if need_dx else None, dim,
-        dgain.data_ptr() if need_params else None, dbias.data_ptr() if need_params else None, gt,
-        ws.data_ptr() if need_params else None, nbytes, s), "tk_layernorm_backward")
+    _enqueue(dev, stream, "tk_layernorm_backward", lib.tk_layernorm_backward, dy.data_ptr(), ds, x.data_ptr(), xs, xt, rows, dim, gp, pt,
+             mp, rp, dxp, dim, dgp, dbp, gt, wsp, nbytes)
     return dx, dgain, dbias
 
 
 def _head(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor):
     if h.dim() != 2 or w.dim() != 2:
         raise ValueError("expected h [tokens][dim] and w [vocab][dim]")
-    (tokens, dim), vocab, dev = h.shape, w.size(0), _cuda_device(h, "h")
-    hs, wst = _matrix(h, tokens, dim, h.dtype, dev, "h"), _matrix(w, vocab, dim, h.dtype, dev, "w")
+    (tokens, dim), vocab, dev, dtype = h.shape, w.shape[0], h.get_device(), h.dtype
+    hs, wst = _matrix(h, tokens, dim, dtype, dev, "h"), _matrix(w, vocab, dim, dtype, dev, "w")
     tp = _vector(target, tokens, torch.int32, dev, "target")
-    aligned = int(h.data_ptr() % 16 == 0 and w.data_ptr() % 16 == 0 and hs % 8 == 0 and wst % 8 == 0)
-    return tokens, vocab, dim, dev, hs, wst, tp, aligned
+    hp, wp = h.data_ptr(), w.data_ptr()
+    aligned = int((hp | wp) % 16 == 0 and (hs | wst) % 8 == 0)
+    return tokens, vocab, dim, dev, hp, hs, wp, wst, tp, aligned
 
 
 def tk_xent_workspace_bytes(tokens: int, vocab: int, dim: int, dtype: torch.dtype, grad_dtype: Optional[torch.dtype] = None,
@@ -532,22 +535,18 @@ def tk_xent_workspace_bytes(tokens: int, vocab: int, dim: int, dtype: torch.dtyp
                                               int(aligned_rows)))
 
 
-def _xent_workspace(h, tokens, vocab, dim, in_type, grad_type, aligned, what):
-    nbytes = load().tk_xent_workspace_bytes(tokens, vocab, dim, in_type, grad_type, aligned)
-    if nbytes == 0:
-        raise TkError(-1, what)
-    return h.new_empty(nbytes, dtype=torch.uint8), nbytes
-
-
 def tk_xent_loss(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(loss, lse) per token of the head h w^T; target int32, negative = takes no part."""
-    tokens, vocab, dim, dev, hs, wst, tp, aligned = _head(h, w, target)
-    it = _type(h.dtype)
+    tokens, vocab, dim, dev, hp, hs, wp, wst, tp, aligned = _head(h, w, target)
+    it, lib = _type(h.dtype), load()
     loss, lse = h.new_empty((2, tokens), dtype=torch.float32).unbind(0)
-    ws, nbytes = _xent_workspace(h, tokens, vocab, dim, it, -1, aligned, "tk_xent_loss")
-    _enqueue(dev, stream, lambda s: load().tk_xent_loss(h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp,
-                                                        loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes, s), "tk_xent_loss")
+    nbytes = lib.tk_xent_workspace_bytes(tokens, vocab, dim, it, -1, aligned)
+    if nbytes == 0:
+        raise TkError(-1, "tk_xent_loss")
+    ws = h.new_empty(nbytes, dtype=torch.uint8)
+    _enqueue(dev, stream, "tk_xent_loss", lib.tk_xent_loss, hp, hs, wp, wst, it, tokens, vocab, dim, tp, loss.data_ptr(), lse.data_ptr(),
+             ws.data_ptr(), nbytes)
     return loss, lse
 
 
@@ -556,20 +555,26 @@ def tk_xent_grad(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor, lse: to
                  need_dh: bool = True, need_dw: bool = True, stream: Optional[torch.cuda.Stream] = None):
     """(dh, dw) of sum_i dloss_i loss_i, from the lse of tk_xent_loss; None for what is not needed.  They are
     made in grad_dtype (default: h's), or written to the given tensors (for example a slice of a gradient row)."""
-    tokens, vocab, dim, dev, hs, wst, tp, aligned = _head(h, w, target)
+    tokens, vocab, dim, dev, hp, hs, wp, wst, tp, aligned = _head(h, w, target)
     if grad_dtype is None:
         grad_dtype = dw.dtype if dw is not None else dh.dtype if dh is not None else h.dtype
-    it, gt = _type(h.dtype), _type(grad_dtype)
+    it, gt, lib = _type(h.dtype), _type(grad_dtype), load()
     lp, dp = _vector(lse, tokens, torch.float32, dev, "lse"), _vector(dloss, tokens, torch.float32, dev, "dloss")
-    dh = (h.new_empty((tokens, dim), dtype=grad_dtype) if dh is None else dh) if need_dh else None
-    dw = (h.new_empty((vocab, dim), dtype=grad_dtype) if dw is None else dw) if need_dw else None
-    dhs = _matrix(dh, tokens, dim, grad_dtype, dev, "dh") if need_dh else 0
-    dws = _matrix(dw, vocab, dim, grad_dtype, dev, "dw") if need_dw else 0
-    ws, nbytes = _xent_workspace(h, tokens, vocab, dim, it, gt, aligned, "tk_xent_grad")
-    _enqueue(dev, stream, lambda s: load().tk_xent_grad(
-        h.data_ptr(), hs, w.data_ptr(), wst, it, tokens, vocab, dim, tp, lp, dp, dh.data_ptr() if need_dh else None, dhs,
-        dw.data_ptr() if need_dw else None, dws, gt, ws.data_ptr(), nbytes, s), "tk_xent_grad")
-    return dh, dw
+    dhs = dws = 0
+    dhp = dwp = None
+    if need_dh:
+        dh = h.new_empty((tokens, dim), dtype=grad_dtype) if dh is None else dh
+        dhs, dhp = _matrix(dh, tokens, dim, grad_dtype, dev, "dh"), dh.data_ptr()
+    if need_dw:
+        dw = h.new_empty((vocab, dim), dtype=grad_dtype) if dw is None else dw
+        dws, dwp = _matrix(dw, vocab, dim, grad_dtype, dev, "dw"), dw.data_ptr()
+    nbytes = lib.tk_xent_workspace_bytes(tokens, vocab, dim, it, gt, aligned)
+    if nbytes == 0:
+        raise TkError(-1, "tk_xent_grad")
+    ws = h.new_empty(nbytes, dtype=torch.uint8)
+    _enqueue(dev, stream, "tk_xent_grad", lib.tk_xent_grad, hp, hs, wp, wst, it, tokens, vocab, dim, tp, lp, dp, dhp, dhs, dwp, dws, gt,
+             ws.data_ptr(), nbytes)
+    return dh if need_dh else None, dw if need_dw else None
 
 
 def tk_xent_status() -> int:
@@ -647,14 +652,14 @@ class AdamW:
         o.grad_type = _type(dtype)
         ptrs = self._pointers(grads, dtype, "grads")
         o.lr, o.grad_scale, o.step = self.lr if lr is None else lr, grad_scale, self.steps + 1
-        _enqueue(self._index, stream, lambda s: load().tk_adamw_step(self._table, ptrs, len(ptrs), ctypes.byref(o), s), "tk_adamw_step")
+        _enqueue(self._index, stream, "tk_adamw_step", load().tk_adamw_step, self._table, ptrs, len(ptrs), ctypes.byref(o))
         self.steps += 1
 
     def tk_adamw_set_state(self, m, v, step: int, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Takes the states from fp32 values, one tensor per parameter (a checkpoint's), and the number of steps done."""
         pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
         if self.state_bits == 8:
-            _enqueue(self._index, stream, lambda s: load().tk_adamw_set_state(self._table, pm, pv, len(pm), s), "tk_adamw_set_state")
+            _enqueue(self._index, stream, "tk_adamw_set_state", load().tk_adamw_set_state, self._table, pm, pv, len(pm))
         else:
             torch._foreach_copy_(list(torch.split(self.m, self.sizes)), [t.reshape(-1) for t in m])
             torch._foreach_copy_(list(torch.split(self.v, self.sizes)), [t.reshape(-1) for t in v])
@@ -664,7 +669,7 @@ class AdamW:
         """Writes the values of the states to fp32 tensors, one per parameter; the number of steps done."""
         pm, pv = self._pointers(m, torch.float32, "m"), self._pointers(v, torch.float32, "v")
         if self.state_bits == 8:
-            _enqueue(self._index, stream, lambda s: load().tk_adamw_get_state(self._table, pm, pv, len(pm), s), "tk_adamw_get_state")
+            _enqueue(self._index, stream, "tk_adamw_get_state", load().tk_adamw_get_state, self._table, pm, pv, len(pm))
         else:
             torch._foreach_copy_([t.view(-1) for t in m], list(torch.split(self.m, self.sizes)))
             torch._foreach_copy_([t.view(-1) for t in v], list(torch.split(self.v, self.sizes)))

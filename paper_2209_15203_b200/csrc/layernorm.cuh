@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kNormFinishCols* kNormFinishSlices)
     __shared__ float part[kNormFinishSlices][kNormFinishCols];
     const int lane = threadIdx.x % kNormFinishCols, slice = threadIdx.x / kNormFinishCols;
     const int64_t c = (int64_t)blockIdx.x * kNormFinishCols + lane;
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // launched while the kernel before may still run
+    wait_for_predecessor();
     float s = 0.0f;
     if (c < 2 * (int64_t)dim) {
         const float* at = partial + (int64_t)slice * 2 * dim + c;

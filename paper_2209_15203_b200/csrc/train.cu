@@ -24,11 +24,11 @@ int launch_error() {
     return TK_OK;
 }
 
-// Launches a kernel that begins with griddepcontrol.wait: its launch overlaps the end of the kernel before it.
+// Launches a kernel that begins with wait_for_predecessor(): its launch overlaps the end of the kernel before it.
 template <typename... KArgs, typename... Args>
-int launch_after(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t stream, Args... args) {
+int launch_after(void (*kernel)(KArgs...), dim3 grid, unsigned block, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -246,7 +246,7 @@ int tk_layernorm_backward(const void* dy, int64_t dy_stride, const void* x, int6
     }
     if (params) {
         const unsigned grid = (unsigned)((2 * dim + kNormFinishCols - 1) / kNormFinishCols);
-        rc = launch_after(norm_finish_kernel, grid, kNormFinishCols * kNormFinishSlices, s, (const float*)workspace, parts, (int)dim,
+        rc = launch_after(norm_finish_kernel, dim3(grid), kNormFinishCols * kNormFinishSlices, s, (const float*)workspace, parts, (int)dim,
                           dgain, dbias, (int)(grad_type == TK_BF16));
     }
     return rc;
@@ -438,13 +438,15 @@ int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
     cfg.blockDim = dim3(kXentThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CG;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (!ready[dev]) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
             cudaGetLastError();
@@ -475,8 +477,8 @@ template <typename T, int PARTS>
 int launch_pack(Device* d, const void* x, int64_t stride, int64_t rows, int64_t dim, int ld, void* out, cudaStream_t s) {
     const int64_t ctas = ceil_div(rows * ld, 256), most = (int64_t)d->sms * 32;
     if (ctas == 0) return TK_OK;
-    xent_pack_kernel<T, PARTS><<<(unsigned)(ctas < most ? ctas : most), 256, 0, s>>>((const T*)x, stride, rows, (int)dim, ld, (bf16*)out);
-    return launch_error();
+    return launch_after(xent_pack_kernel<T, PARTS>, dim3((unsigned)(ctas < most ? ctas : most)), 256, s, (const T*)x, stride, rows, (int)dim,
+                        ld, (bf16*)out);
 }
 
 // The product's rounds in items of at most `per` (0: all), those in accumulation chunks of equal length, at most `most`
@@ -490,8 +492,7 @@ void set_rounds(XentProblem& p, int per, int most) {
 
 int launch_join_tiles(const XentProblem& p, int rows, cudaStream_t s) {
     if (p.splits == 1) return TK_OK;
-    xent_join_tiles_kernel<<<dim3((unsigned)(p.tiles_m * p.tiles_n), kJoinSlices), 256, 0, s>>>(p, rows);
-    return launch_error();
+    return launch_after(xent_join_tiles_kernel, dim3((unsigned)(p.tiles_m * p.tiles_n), kJoinSlices), 256, s, p, rows);
 }
 
 struct XentInputs {
@@ -569,9 +570,8 @@ int tk_xent_loss(const void* h, int64_t h_stride, const void* w, int64_t w_strid
     // of 394 half tiles, a chain of loads)
     const int lanes = tokens >= 512 ? 8 : 32;
     const int64_t warps = (tokens + 32 / lanes - 1) / (32 / lanes);
-    xent_join_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a.partial, a.picked, target, (int)tokens, (int)vocab, 2 * L.tiles_v, lanes,
-                                                                 loss, lse);
-    return launch_error();
+    return launch_after(xent_join_kernel, dim3((unsigned)((warps + 7) / 8)), 256, s, a.partial, a.picked, target, (int)tokens, (int)vocab,
+                        2 * p.tiles_n, lanes, loss, lse);
 }
 
 int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type, int64_t tokens, int64_t vocab,

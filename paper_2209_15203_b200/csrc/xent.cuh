@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
     if (CG == 2) cluster_sync();
     tcgen05_fence_after();
     const u32 tmem = *(volatile u32*)(sm + (tmem_slot - base));
+    wait_for_predecessor();
 
     // 384 threads x 168 registers at launch; the epilogue's two warpgroups take over what the first gives up
     // (128 x 56 + 256 x 216 = 62,464 of 64,512)
@@ -461,6 +462,7 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
 // Adds up the items of each tile in the order of their rounds, and what the earlier pieces of the vocabulary left.
 constexpr int kJoinSlices = 8;
 __global__ void __launch_bounds__(256) xent_join_tiles_kernel(const __grid_constant__ XentProblem P, int rows) {
+    wait_for_predecessor();
     const int m = blockIdx.x / P.tiles_n, n = blockIdx.x % P.tiles_n;
     const int quads = rows * kTileN / 4 / kJoinSlices;   // a multiple of 1024
     const float4* head = (const float4*)(P.part + (int64_t)blockIdx.x * rows * kTileN);
@@ -502,6 +504,7 @@ __global__ void __launch_bounds__(256) xent_join_tiles_kernel(const __grid_const
 // Joins the tiles of each row: lse and loss.  `lanes` (a power of two up to 32) threads per row.
 __global__ void __launch_bounds__(256) xent_join_kernel(const float2* partial, const float* picked, const int* target, int tokens,
                                                         int vocab, int tiles, int lanes, float* loss, float* lse) {
+    wait_for_predecessor();
     // the lanes of a warp lie side by side along the rows: four rows make a sector of 32 bytes
     const int rows = 32 / lanes;
     const int warp = (int)((blockIdx.x * 256 + threadIdx.x) >> 5), lane = threadIdx.x & 31;
@@ -542,6 +545,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* partial, c
 template <typename T, int PARTS>
 __global__ void __launch_bounds__(256) xent_pack_kernel(const T* x, int64_t stride, int64_t rows, int dim, int ld, bf16* out) {
     const int64_t n = rows * ld, step = (int64_t)gridDim.x * 256;
+    wait_for_predecessor();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
         const int64_t r = i / ld;
         const int c = (int)(i - r * ld);
