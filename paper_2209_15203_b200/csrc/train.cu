@@ -473,14 +473,6 @@ int launch_xent(Device* d, int cg, const XentArgs& a, cudaStream_t s) {
     return cg == 2 ? launch_xent<MODE, 2, PARTS>(d, a, s) : launch_xent<MODE, 1, PARTS>(d, a, s);
 }
 
-template <typename T, int PARTS>
-int launch_pack(Device* d, const void* x, int64_t stride, int64_t rows, int64_t dim, int ld, void* out, cudaStream_t s) {
-    const int64_t ctas = ceil_div(rows * ld, 256), most = (int64_t)d->sms * 32;
-    if (ctas == 0) return TK_OK;
-    return launch_after(xent_pack_kernel<T, PARTS>, dim3((unsigned)(ctas < most ? ctas : most)), 256, s, (const T*)x, stride, rows, (int)dim,
-                        ld, (bf16*)out);
-}
-
 // The product's rounds in items of at most `per` (0: all), those in accumulation chunks of equal length, at most `most`
 // rounds (0: all).
 void set_rounds(XentProblem& p, int per, int most) {
@@ -492,7 +484,8 @@ void set_rounds(XentProblem& p, int per, int most) {
 
 int launch_join_tiles(const XentProblem& p, int rows, cudaStream_t s) {
     if (p.splits == 1) return TK_OK;
-    return launch_after(xent_join_tiles_kernel, dim3((unsigned)(p.tiles_m * p.tiles_n), kJoinSlices), 256, s, p, rows);
+    return launch_after(xent_join_tiles_kernel, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)(rows * kTileN / 4 / kJoinQuads)), kJoinQuads, s,
+                        p, rows);
 }
 
 struct XentInputs {
@@ -501,6 +494,13 @@ struct XentInputs {
 };
 
 // Copies the inputs to the workspace if the kernel cannot read them where they are.
+template <typename T, int PARTS>
+int launch_pack(Device* d, const XentLayout& L, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int64_t tokens,
+                int64_t vocab, int64_t dim, char* ws, cudaStream_t s) {
+    const PackInput<T> first = {(const T*)h, h_stride, tokens, (bf16*)(ws + L.off_h)}, second = {(const T*)w, w_stride, vocab, (bf16*)(ws + L.off_w)};
+    const int64_t ctas = ceil_div(tokens + vocab, 8), most = (int64_t)d->sms * 8;
+    return launch_after(xent_pack_kernel<T, PARTS>, dim3((unsigned)(ctas < most ? ctas : most)), 256, s, first, second, (int)dim, L.ld);
+}
 int xent_inputs(Device* d, const XentLayout& L, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type,
                 int64_t tokens, int64_t vocab, int64_t dim, char* ws, XentInputs* out, cudaStream_t s) {
     if (!L.pack) {
@@ -508,15 +508,8 @@ int xent_inputs(Device* d, const XentLayout& L, const void* h, int64_t h_stride,
         return TK_OK;
     }
     *out = {ws + L.off_h, ws + L.off_w, L.ld, L.ld};
-    int rc;
-    if (in_type == TK_F32) {
-        rc = launch_pack<float, 3>(d, h, h_stride, tokens, dim, L.ld, ws + L.off_h, s);
-        if (rc == TK_OK) rc = launch_pack<float, 3>(d, w, w_stride, vocab, dim, L.ld, ws + L.off_w, s);
-    } else {
-        rc = launch_pack<bf16, 1>(d, h, h_stride, tokens, dim, L.ld, ws + L.off_h, s);
-        if (rc == TK_OK) rc = launch_pack<bf16, 1>(d, w, w_stride, vocab, dim, L.ld, ws + L.off_w, s);
-    }
-    return rc;
+    if (in_type == TK_F32) return launch_pack<float, 3>(d, L, h, h_stride, w, w_stride, tokens, vocab, dim, ws, s);
+    return launch_pack<bf16, 1>(d, L, h, h_stride, w, w_stride, tokens, vocab, dim, ws, s);
 }
 
 bool xent_rows_aligned(const void* p, int64_t stride) { return aligned(p, 16) && stride % 8 == 0; }

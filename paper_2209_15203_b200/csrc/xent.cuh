@@ -428,8 +428,13 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                 float* sum = whole ? P.acc + (int64_t)m0 * P.cols + n0
                                    : P.part + (((int64_t)t.split * P.tiles_m + t.m) * P.tiles_n + t.n) * kTileM * CG * kTileN +
                                          ((int)rank * kTileM + 32 * quarter) * kTileN + half * kEpiCols;
-                const int pitch = whole ? P.cols : kTileN;
-                const bool read = whole && P.acc_read, write = !whole || P.acc_write, out = whole && P.out;
+                const int64_t pitch = whole ? P.cols : kTileN, ld = P.ld;
+                const bool read = whole && P.acc_read, write = !whole || P.acc_write;
+                void* out = whole ? P.out : nullptr;
+                const bool out_bf16 = P.out_bf16;
+                if (out) out = (char*)out + ((int64_t)m0 * ld + n0) * (out_bf16 ? 2 : 4);
+                // 32 columns at a time across the warp, so that a row's stores are one line; 16 rows are read back before the
+                // first is stored (one by one, a tile took 25,000 cycles, and fp32 gradients waited for it)
 #pragma unroll
                 for (int c = 0; c < kEpiCols; c += 32) {
                     __syncwarp();
@@ -437,14 +442,33 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                     for (int i = 0; i < 32; ++i) stage_ptr[lane * 33 + i] = v[c + i];
                     __syncwarp();
                     if (c + lane < cols) {
-                        float* to = sum + c + lane;
-                        int64_t at = (int64_t)m0 * P.ld + n0 + c + lane;
-#pragma unroll 4
-                        for (int r = 0; r < rows; ++r, to += pitch, at += P.ld) {
-                            float x = stage_ptr[r * 33 + lane];
-                            if (read) x += *to;
-                            if (write) *to = x;
-                            if (out) store_any(P.out, at, x, P.out_bf16);
+#pragma unroll 1
+                        for (int r0 = 0; r0 < rows; r0 += 16) {
+                            float x[16];
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) x[r] = stage_ptr[(r0 + r) * 33 + lane];
+                            float* to = sum + r0 * pitch + c + lane;
+                            if (read) {
+#pragma unroll
+                                for (int r = 0; r < 16; ++r)
+                                    if (r0 + r < rows) x[r] += to[r * pitch];
+                            }
+                            if (write) {
+#pragma unroll
+                                for (int r = 0; r < 16; ++r)
+                                    if (r0 + r < rows) to[r * pitch] = x[r];
+                            }
+                            if (out && out_bf16) {
+                                bf16* o = (bf16*)out + r0 * ld + c + lane;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r)
+                                    if (r0 + r < rows) o[r * ld] = from_float<bf16>(x[r]);
+                            } else if (out) {
+                                float* o = (float*)out + r0 * ld + c + lane;
+#pragma unroll
+                                for (int r = 0; r < 16; ++r)
+                                    if (r0 + r < rows) o[r * ld] = x[r];
+                            }
                         }
                     }
                 }
@@ -459,45 +483,41 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
     if (warp == 2) tmem_free<CG>(tmem, 512);
 }
 
-// Adds up the items of each tile in the order of their rounds, and what the earlier pieces of the vocabulary left.
-constexpr int kJoinSlices = 8;
-__global__ void __launch_bounds__(256) xent_join_tiles_kernel(const __grid_constant__ XentProblem P, int rows) {
+// Adds up the items of each tile in the order of their rounds, and what the earlier pieces of the vocabulary left.  A
+// thread has four neighbouring columns and eight items in flight.
+constexpr int kJoinQuads = 256;   // per CTA
+__global__ void __launch_bounds__(kJoinQuads) xent_join_tiles_kernel(const __grid_constant__ XentProblem P, int rows) {
     wait_for_predecessor();
     const int m = blockIdx.x / P.tiles_n, n = blockIdx.x % P.tiles_n;
-    const int quads = rows * kTileN / 4 / kJoinSlices;   // a multiple of 1024
-    const float4* head = (const float4*)(P.part + (int64_t)blockIdx.x * rows * kTileN);
-    const int64_t next_split = (int64_t)gridDim.x * rows * kTileN / 4;
-    for (int i0 = blockIdx.y * quads + threadIdx.x; i0 < (blockIdx.y + 1) * quads; i0 += 1024) {
-        float4 x[4];
+    const int i = blockIdx.y * kJoinQuads + threadIdx.x;   // of rows * 64 groups of four columns
+    const int64_t r = (int64_t)m * rows + i / (kTileN / 4);
+    const int c = n * kTileN + i % (kTileN / 4) * 4;
+    if (r >= P.rows || c >= P.cols) return;
+    const float4* at = (const float4*)(P.part + (int64_t)blockIdx.x * rows * kTileN) + i;
+    const int64_t step = (int64_t)gridDim.x * rows * kTileN / 4;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < P.splits; k += 8, at += 8 * step) {
+        float4 q[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = head[i0 + 256 * j];
-        const float4* next = head;
-        for (int k = 1; k < P.splits; ++k) {
-            next += next_split;
+        for (int j = 0; j < 8; ++j)
+            if (k + j < P.splits) q[j] = at[j * step];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 q = next[i0 + 256 * j];
-                x[j].x += q.x;
-                x[j].y += q.y;
-                x[j].z += q.z;
-                x[j].w += q.w;
+        for (int j = 0; j < 8; ++j)
+            if (k + j < P.splits) {
+                x.x += q[j].x;
+                x.y += q[j].y;
+                x.z += q[j].z;
+                x.w += q[j].w;
             }
-        }
+    }
+    const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = i0 + 256 * j;
-            const int64_t r = (int64_t)m * rows + i / (kTileN / 4);
-            const int c = n * kTileN + i % (kTileN / 4) * 4;
-            const float y[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (r >= P.rows || c + e >= P.cols) continue;
-                float v = y[e];
-                if (P.acc_read) v += P.acc[r * P.cols + c + e];
-                if (P.acc_write) P.acc[r * P.cols + c + e] = v;
-                if (P.out) store_any(P.out, r * P.ld + c + e, v, P.out_bf16);
-            }
-        }
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= P.cols) break;
+        float v = y[e];
+        if (P.acc_read) v += P.acc[r * P.cols + c + e];
+        if (P.acc_write) P.acc[r * P.cols + c + e] = v;
+        if (P.out) store_any(P.out, r * P.ld + c + e, v, P.out_bf16);
     }
 }
 
@@ -541,20 +561,36 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* partial, c
     }
 }
 
-// An operand [rows][dim] as PARTS bf16 matrices [rows][ld] (zeros beyond dim).
+// An operand [rows][dim] as PARTS bf16 matrices [rows][ld] (zeros beyond dim; ld is a multiple of 8): one warp per row and 256
+// columns, eight neighbouring ones per thread; ahead of that the second operand's rows, if there is one.
+template <typename T> struct PackInput {
+    const T* x;
+    int64_t stride, rows;
+    bf16* out;
+};
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(256) xent_pack_kernel(const T* x, int64_t stride, int64_t rows, int dim, int ld, bf16* out) {
-    const int64_t n = rows * ld, step = (int64_t)gridDim.x * 256;
+__global__ void __launch_bounds__(256) xent_pack_kernel(const PackInput<T> first, const PackInput<T> second, int dim, int ld) {
     wait_for_predecessor();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
-        const int64_t r = i / ld;
-        const int c = (int)(i - r * ld);
-        float v = c < dim ? to_float(x[r * stride + c]) : 0.0f;
+    const int64_t warps = (int64_t)gridDim.x * 8;
+    const int lane = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < first.rows + second.rows; row += warps) {
+        const bool one = row < first.rows;
+        const int64_t r = one ? row : row - first.rows, rows = one ? first.rows : second.rows;
+        const T* x = (one ? first.x : second.x) + r * (one ? first.stride : second.stride);
+        bf16* out = (one ? first.out : second.out) + r * ld;
+        for (int c = lane * 8; c < ld; c += 256) {
+            float v[8];
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            bf16 q = from_float<bf16>(v);
-            out[p * n + i] = q;
-            v -= to_float(q);
+            for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? to_float(x[c + i]) : 0.0f;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                uint4 q;
+                q.x = take_part(v[0], v[1], p == PARTS - 1);
+                q.y = take_part(v[2], v[3], p == PARTS - 1);
+                q.z = take_part(v[4], v[5], p == PARTS - 1);
+                q.w = take_part(v[6], v[7], p == PARTS - 1);
+                *(uint4*)(out + p * rows * ld + c) = q;
+            }
         }
     }
 }
