@@ -559,9 +559,9 @@ int tk_xent_loss(const void* h, int64_t h_stride, const void* w, int64_t w_strid
     a.status = d->status;
     rc = launch_xent<kXentLoss, 1>(d, L.cg, a, s);
     if (rc != TK_OK) return rc;
-    // few rows: a warp per row; else 8 lanes per row, whose loads are whole sectors (one lane per row took 65 us for 8192 rows
-    // of 394 half tiles, a chain of loads)
-    const int lanes = tokens >= 512 ? 8 : 32;
+    // Lanes per row: 8 read whole sectors, 32 leave each the fewest loads in a row.  1000 tokens x 394 half tiles: 9.7 us with 8, 6.4 with
+    // 32; 8192 tokens: 11.3 and 16.4 (a lane per row took 65 us there).
+    const int lanes = tokens >= 4096 ? 8 : 32;
     const int64_t warps = (tokens + 32 / lanes - 1) / (32 / lanes);
     return launch_after(xent_join_kernel, dim3((unsigned)((warps + 7) / 8)), 256, s, a.partial, a.picked, target, (int)tokens, (int)vocab,
                         2 * p.tiles_n, lanes, loss, lse);
