@@ -15,7 +15,7 @@
 // Operands are bf16.  An fp32 operand is held as three bf16 parts, hi + mid + lo, which represent it
 // exactly, and a product takes the part pairs of order up to 2^-16 (six of nine; three when the other
 // operand is bf16): what is left out is below fp32's own rounding.  D is one part when the gradients are
-// bf16 (a rounding of 2^-9 of each coefficient, as in any 16-bit training step) and three when they are fp32.
+// bf16 (a rounding of at most 2^-8 of each coefficient, as in any 16-bit training step) and three when they are fp32.
 //
 // One CTA (CG 1) or pair (CG 2) per SM (pair) is persistent over tiles of 128 CG x 256: one thread issues TMA
 // loads into a ring of stages of 64 of K, one issues the matrix instructions into one of two accumulators
@@ -26,8 +26,15 @@
 // sum, always towards zero (measured: 2e-8 of a sum per 16 products, 1.2e-5 over 10,007 of them).  Results that
 // are to be good to fp32 are therefore summed in chunks of at most kChunk blocks of 64 products, added
 // up in registers with correct rounding.
+//
 // Both gradient products read D or w or h along the dimension that is not contiguous; the matrix
 // instructions take such operands ("MN-major") directly, so nothing is transposed in memory.
+//
+// Bound by the matrix pipe, and in long runs by the power limit behind it; for few tokens by reading w.  Measured on one B200
+// (bf16): 4096 tokens x 131,072 x 2048, loss 1332 us (1652 TFLOP/s, matrix pipe active 94 % of the cycles), a piece's D
+// 333 us, its two products 718 us; loss and gradient together 5.74 ms alone, 6.66 ms back to back at the power limit (1322 TFLOP/s of
+// the 8 flops per token, entry and dim).  8192 x 50,257 x 768: loss 406 us, D 5 x 93 us, products 5 x 175 us.  61 tokens x 50,257 x 768: 22 us
+// (3.5 TB/s of w; the second round of tiles fills a third of the SMs).
 #pragma once
 
 #include "tcgen05.cuh"
