@@ -424,7 +424,7 @@ def _type(dtype: torch.dtype) -> int:
 
 def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: int, what: str) -> int:
     """Checks a [rows][dim] matrix whose rows are contiguous, on CUDA device `device`; its row stride in values."""
-    if t.shape != (rows, dim) or t.dtype != dtype or t.get_device() != device:
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (rows, dim):
         raise ValueError("%s: expected a [%d][%d] tensor of %s on the inputs' CUDA device" % (what, rows, dim, dtype))
     if t.is_contiguous():
         return dim
@@ -437,7 +437,7 @@ def _matrix(t: torch.Tensor, rows: int, dim: int, dtype: torch.dtype, device: in
 
 
 def _vector(t: torch.Tensor, n: int, dtype: torch.dtype, device: int, what: str) -> int:
-    if t.shape != (n,) or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s: expected a contiguous [%d] tensor of %s on the inputs' CUDA device" % (what, n, dtype))
     return t.data_ptr()
 
@@ -473,10 +473,11 @@ def tk_layernorm_forward(x: torch.Tensor, gain: torch.Tensor, bias: Optional[tor
     xt, pt = _type(dtype), _type(param)
     xs, gp = _matrix(x, rows, dim, dtype, dev, "x"), _vector(gain, dim, param, dev, "gain")
     bp = _vector(bias, dim, param, dev, "bias") if bias is not None else None
-    y = x.new_empty((rows, dim))
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+    mp = mean.data_ptr()
     _enqueue(dev, stream, "tk_layernorm_forward", load().tk_layernorm_forward, x.data_ptr(), xt, rows, dim, xs, gp, bp, pt, eps,
-             y.data_ptr(), dim, mean.data_ptr(), rstd.data_ptr())
+             y.data_ptr(), dim, mp, mp + 4 * rows)
     return y, mean, rstd
 
 
@@ -496,25 +497,25 @@ def tk_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
     gp = _vector(gain, dim, param, dev, "gain")
     mp, rp = _vector(mean, rows, torch.float32, dev, "mean"), _vector(rstd, rows, torch.float32, dev, "rstd")
     lib = load()
-    dx, dxp = None, None
-    if need_dx:
-        dx = x.new_empty((rows, dim))
-        dxp = dx.data_ptr()
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
     dgp = dbp = wsp = None
     nbytes = 0
     if need_params:
-        if dgain is None and dbias is None:
-            dgain, dbias = x.new_empty((2, dim), dtype=grad_dtype).unbind(0)
-        dgain = x.new_empty(dim, dtype=grad_dtype) if dgain is None else dgain
-        dbias = x.new_empty(dim, dtype=grad_dtype) if dbias is None else dbias
-        dgp, dbp = _vector(dgain, dim, grad_dtype, dev, "dgain"), _vector(dbias, dim, grad_dtype, dev, "dbias")
         nbytes = lib.tk_layernorm_workspace_bytes(rows, dim)
         ws = x.new_empty(nbytes, dtype=torch.uint8)
         wsp = ws.data_ptr()
+        if dgain is None and dbias is None:
+            dgain, dbias = x.new_empty((2, dim), dtype=grad_dtype).unbind(0)
+            dgp = dgain.data_ptr()
+            dbp = dgp + dim * grad_dtype.itemsize
+        else:
+            dgain = x.new_empty(dim, dtype=grad_dtype) if dgain is None else dgain
+            dbias = x.new_empty(dim, dtype=grad_dtype) if dbias is None else dbias
+            dgp, dbp = _vector(dgain, dim, grad_dtype, dev, "dgain"), _vector(dbias, dim, grad_dtype, dev, "dbias")
     else:
         dgain = dbias = None
     _enqueue(dev, stream, "tk_layernorm_backward", lib.tk_layernorm_backward, dy.data_ptr(), ds, x.data_ptr(), xs, xt, rows, dim, gp, pt,
-             mp, rp, dxp, dim, dgp, dbp, gt, wsp, nbytes)
+             mp, rp, dx.data_ptr() if need_dx else None, dim, dgp, dbp, gt, wsp, nbytes)
     return dx, dgain, dbias
 
 
@@ -541,11 +542,12 @@ def tk_xent_loss(h: torch.Tensor, w: torch.Tensor, target: torch.Tensor,
     tokens, vocab, dim, dev, hp, hs, wp, wst, tp, aligned = _head(h, w, target)
     it, lib = _type(h.dtype), load()
     loss, lse = h.new_empty((2, tokens), dtype=torch.float32).unbind(0)
+    lp = loss.data_ptr()
     nbytes = lib.tk_xent_workspace_bytes(tokens, vocab, dim, it, -1, aligned)
     if nbytes == 0:
         raise TkError(-1, "tk_xent_loss")
     ws = h.new_empty(nbytes, dtype=torch.uint8)
-    _enqueue(dev, stream, "tk_xent_loss", lib.tk_xent_loss, hp, hs, wp, wst, it, tokens, vocab, dim, tp, loss.data_ptr(), lse.data_ptr(),
+    _enqueue(dev, stream, "tk_xent_loss", lib.tk_xent_loss, hp, hs, wp, wst, it, tokens, vocab, dim, tp, lp, lp + 4 * tokens,
              ws.data_ptr(), nbytes)
     return loss, lse
 
