@@ -448,10 +448,13 @@ int launch_xent(Device* d, const XentArgs& a, cudaStream_t s) {
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     if (!ready[dev]) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+        cudaFuncAttributes built;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+            cudaFuncGetAttributes(&built, kernel) != cudaSuccess) {
             cudaGetLastError();
             return TK_ERR_CUDA;
         }
+        if (built.numRegs * kXentThreads < kSplitRegs) return TK_ERR_INTERNAL;
         cfg.gridDim = dim3((unsigned)(d->sms / CG * CG));
         if (cudaOccupancyMaxActiveClusters(&pairs[dev], kernel, &cfg) != cudaSuccess || pairs[dev] < 1) {
             cudaGetLastError();
@@ -612,7 +615,6 @@ int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_strid
         soft.tokens = (int)tokens, soft.vocab = (int)vocab, soft.target = target, soft.lse = lse, soft.dloss = dloss;
         soft.status = grad.status = d->status;
         soft.panels = grad.panels = panels;
-        grad.tokens = (int)tokens, grad.vocab = (int)vocab;
     }
     XentProblem pw = {}, ph = {};
     if (dw) {   // dw[v][:] = sum over tokens of D[t][v] h[t][:]

@@ -46,6 +46,10 @@ enum { kXentLoss = 0, kXentSoft = 1, kXentGrad = 2 };
 constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
 constexpr int kXentThreads = 384;   // warps: TMA, matrix instructions, tensor memory, -, 8 x epilogue
 constexpr int kXentEpiWarp = 4, kXentEpiWarps = 8;
+// Registers per thread after the split of the launch's: the first warpgroup gives up what the epilogue's two take over.  A split that
+// asks for more than the launch has would wait forever, so the host checks the sum against the kernel's (168 x 384 = 64,512).
+constexpr int kIssueRegs = 56, kEpiRegs = 216;
+constexpr int kSplitRegs = 32 * (kXentEpiWarp * kIssueRegs + kXentEpiWarps * kEpiRegs);
 constexpr int kEpiCols = 128;       // columns an epilogue thread holds
 // Blocks of 64 products summed in tensor memory where fp32 accuracy is wanted: in the loss and in the products of fp32 gradients.
 // Loss and gradient take the same, so that what truncation is left in l cancels in exp(l - lse).
@@ -70,8 +74,8 @@ struct alignas(64) XentProblem {
     int cols;                 // columns of the result
     int a_mn;                 // kGrad: A is MN-major (dw); B always is
     int b_panels;             // kGrad: B's map is in panels of 64 columns and one load brings all of a stage's (rows of whole panels)
-    int a_off, b_off;         // first row (M, N) within the operand's map
-    int a_koff, b_koff;       // first K within the operand's map
+    int b_off;                // kSoft: first row of B (a vocabulary entry) within its map
+    int b_koff;               // kGrad: first K of B within its map
     int nseg;                 // part pairs, smallest products first
     unsigned char sa[6], sb[6];
     // kGrad: where the tile goes
@@ -202,96 +206,94 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
     const u32 tmem = *(volatile u32*)(sm + (tmem_slot - base));
     wait_for_predecessor();
 
-    // 384 threads x 168 registers at launch; the epilogue's two warpgroups take over what the first gives up
-    // (128 x 56 + 256 x 216 = 62,464 of 64,512)
     if (warp < kXentEpiWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 && lane == 0) {
-        // ---- loads ----
-        const u32 full0 = CG == 2 ? mapped_addr(full, 0) : full;   // both CTAs' copies report to the leader
-        u32 it = 0;
-        bool ok = true;
-        for (u32 id = worker; ok && id < A.items; id += workers) {
-            const XentItem t = xent_item<MODE>(A, id);
-            const XentProblem& P = A.p[t.problem];
-            const int mine = xent_columns<MODE, CG>(P, t.n) / CG;
-            const int a0 = P.a_off + (t.m * CG + (int)rank) * kTileM, b0 = P.b_off + t.n * kTileN + (int)rank * mine;
-            const int boxes = MODE == kXentGrad ? (P.b_panels ? S::kBRows / 64 : (mine + 63) / 64) : 0;
-            const u32 bytes = kABytes + (MODE == kXentGrad ? boxes * kBoxBytes : S::kBRows * kTileK * 2);
-            // the loop below has half a microsecond per round: nothing of it is looked up in the parameters
-            const int kblocks = P.kblocks, a_koff = P.a_koff, b_koff = P.b_koff, a_mn = P.a_mn, b_panels = P.b_panels, panels = A.panels;
-            const CUtensorMap *map_a = &P.a, *map_b = &P.b;
-            int seg = t.r0 / kblocks, k = t.r0 % kblocks;
-            for (int r = t.r0; r < t.r1;) {
-                const int pa = P.sa[seg], pb = P.sb[seg];
-                ++seg;
-                for (; k < kblocks && r < t.r1; ++k, ++r, ++it) {
-                    const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
-                    if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1))) break;
-                    const u32 a = base + stage * S::kStageBytes, b = a + kABytes, bar = full0 + 8 * stage;
-                    if (rank == 0) mbar_expect(full + 8 * stage, bytes * CG);
-                    const int ka = a_koff + k * kTileK, kb = b_koff + k * kTileK;
-                    if (MODE != kXentGrad) {
-                        tma_load<CG>(a, map_a, bar, ka, a0, pa);
-                        tma_load<CG>(b, map_b, bar, kb, b0, pb);
-                    } else {
-                        if (a_mn) {   // D: panels of 64 vocabulary entries
-                            tma_load<CG>(a, map_a, bar, 0, ka, a0 / 64 + pa * panels);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+        if (warp == 0 && lane == 0) {
+            // ---- loads ----
+            const u32 full0 = CG == 2 ? mapped_addr(full, 0) : full;   // both CTAs' copies report to the leader
+            u32 it = 0;
+            bool ok = true;
+            for (u32 id = worker; ok && id < A.items; id += workers) {
+                const XentItem t = xent_item<MODE>(A, id);
+                const XentProblem& P = A.p[t.problem];
+                const int mine = xent_columns<MODE, CG>(P, t.n) / CG;
+                const int a0 = (t.m * CG + (int)rank) * kTileM, b0 = P.b_off + t.n * kTileN + (int)rank * mine;
+                const int boxes = MODE == kXentGrad ? (P.b_panels ? S::kBRows / 64 : (mine + 63) / 64) : 0;
+                const u32 bytes = kABytes + (MODE == kXentGrad ? boxes * kBoxBytes : S::kBRows * kTileK * 2);
+                // the loop below has half a microsecond per round: nothing of it is looked up in the parameters
+                const int kblocks = P.kblocks, b_koff = P.b_koff, a_mn = P.a_mn, b_panels = P.b_panels, panels = A.panels;
+                const CUtensorMap *map_a = &P.a, *map_b = &P.b;
+                int seg = t.r0 / kblocks, k = t.r0 % kblocks;
+                for (int r = t.r0; r < t.r1;) {
+                    const int pa = P.sa[seg], pb = P.sb[seg];
+                    ++seg;
+                    for (; k < kblocks && r < t.r1; ++k, ++r, ++it) {
+                        const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
+                        if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1))) break;
+                        const u32 a = base + stage * S::kStageBytes, b = a + kABytes, bar = full0 + 8 * stage;
+                        if (rank == 0) mbar_expect(full + 8 * stage, bytes * CG);
+                        const int ka = k * kTileK, kb = b_koff + k * kTileK;
+                        if (MODE != kXentGrad) {
+                            tma_load<CG>(a, map_a, bar, ka, a0, pa);
+                            tma_load<CG>(b, map_b, bar, kb, b0, pb);
                         } else {
-                            tma_load<CG>(a, map_a, bar, 0, a0, k + pa * panels);
+                            if (a_mn) {   // D: panels of 64 vocabulary entries
+                                tma_load<CG>(a, map_a, bar, 0, ka, a0 / 64 + pa * panels);
+                            } else {
+                                tma_load<CG>(a, map_a, bar, 0, a0, k + pa * panels);
+                            }
+                            if (b_panels)
+                                tma_load4<CG>(b, map_b, bar, 0, kb, b0 / 64, pb);
+                            else
+                                for (int j = 0; j < boxes; ++j) tma_load<CG>(b + j * kBoxBytes, map_b, bar, b0 + 64 * j, kb, pb);
                         }
-                        if (b_panels)
-                            tma_load4<CG>(b, map_b, bar, 0, kb, b0 / 64, pb);
-                        else
-                            for (int j = 0; j < boxes; ++j) tma_load<CG>(b + j * kBoxBytes, map_b, bar, b0 + 64 * j, kb, pb);
                     }
+                    if (!ok) break;
+                    k = 0;
                 }
-                if (!ok) break;
-                k = 0;
             }
-        }
-        // nothing of this CTA is in flight when it ends: every stage that was filled has been consumed
-        for (u32 i = it > (u32)S::kStages ? it - S::kStages : 0; i < it; ++i)
-            if (!mbar_wait(empty + 8 * (i % S::kStages), (i / S::kStages) & 1)) ok = false;
-        if (!ok) atomicExch(A.status, 1);
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-        // ---- matrix instructions ----
-        u32 it = 0, turn = 0;
-        bool ok = true;
-        for (u32 id = worker; ok && id < A.items; id += workers) {
-            const XentItem t = xent_item<MODE>(A, id);
-            const XentProblem& P = A.p[t.problem];
-            const bool a_mn = MODE == kXentGrad && P.a_mn, b_mn = MODE == kXentGrad;
-            const u32 desc = mma_desc(kTileM * CG, xent_columns<MODE, CG>(P, t.n), a_mn, b_mn);
-            const u64 step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4;
-            const u64 first_a = smem_desc(base, a_mn ? kBoxBytes : 0, 1024), first_b = smem_desc(base + kABytes, b_mn ? kBoxBytes : 0, 1024);
-            const int rounds = t.r1 - t.r0, chunk = P.chunk;
-            for (int r0 = 0; ok && r0 < rounds; r0 += chunk, ++turn) {
-                const u32 slot = turn & 1, acc = tmem + slot * kTileN;
-                if (!(ok = mbar_wait(freed + 8 * slot, ((turn >> 1) & 1) ^ 1))) break;
-                tcgen05_fence_after();
-                const int n = min(chunk, rounds - r0);
-                for (int k = 0; k < n; ++k, ++it) {
-                    const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
-                    if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+            // nothing of this CTA is in flight when it ends: every stage that was filled has been consumed
+            for (u32 i = it > (u32)S::kStages ? it - S::kStages : 0; i < it; ++i)
+                if (!mbar_wait(empty + 8 * (i % S::kStages), (i / S::kStages) & 1)) ok = false;
+            if (!ok) atomicExch(A.status, 1);
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            // ---- matrix instructions ----
+            u32 it = 0, turn = 0;
+            bool ok = true;
+            for (u32 id = worker; ok && id < A.items; id += workers) {
+                const XentItem t = xent_item<MODE>(A, id);
+                const XentProblem& P = A.p[t.problem];
+                const bool a_mn = MODE == kXentGrad && P.a_mn, b_mn = MODE == kXentGrad;
+                const u32 desc = mma_desc(kTileM * CG, xent_columns<MODE, CG>(P, t.n), a_mn, b_mn);
+                const u64 step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4;
+                const u64 first_a = smem_desc(base, a_mn ? kBoxBytes : 0, 1024), first_b = smem_desc(base + kABytes, b_mn ? kBoxBytes : 0, 1024);
+                const int rounds = t.r1 - t.r0, chunk = P.chunk;
+                for (int r0 = 0; ok && r0 < rounds; r0 += chunk, ++turn) {
+                    const u32 slot = turn & 1, acc = tmem + slot * kTileN;
+                    if (!(ok = mbar_wait(freed + 8 * slot, ((turn >> 1) & 1) ^ 1))) break;
                     tcgen05_fence_after();
-                    const u64 da = first_a + stage * (S::kStageBytes >> 4), db = first_b + stage * (S::kStageBytes >> 4);
+                    const int n = min(chunk, rounds - r0);
+                    for (int k = 0; k < n; ++k, ++it) {
+                        const u32 stage = it % S::kStages, phase = (it / S::kStages) & 1;
+                        if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+                        tcgen05_fence_after();
+                        const u64 da = first_a + stage * (S::kStageBytes >> 4), db = first_b + stage * (S::kStageBytes >> 4);
 #pragma unroll
-                    for (int i = 0; i < kTileK / 16; ++i) mma_bf16<CG>(acc, da + i * step_a, db + i * step_b, desc, k > 0 || i > 0);
-                    mma_commit<CG>(empty + 8 * stage);
+                        for (int i = 0; i < kTileK / 16; ++i) mma_bf16<CG>(acc, da + i * step_a, db + i * step_b, desc, k > 0 || i > 0);
+                        mma_commit<CG>(empty + 8 * stage);
+                    }
+                    if (ok) mma_commit<CG>(done + 8 * slot);
                 }
-                if (ok) mma_commit<CG>(done + 8 * slot);
+            }
+            if (!ok) {
+                mma_commit<CG>(drain);
+                mbar_wait(drain, 0);
+                atomicExch(A.status, 1);
             }
         }
-        if (!ok) {
-            mma_commit<CG>(drain);
-            mbar_wait(drain, 0);
-            atomicExch(A.status, 1);
-        }
-    }
     } else {
         // ---- accumulators to their destination ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
         const int w = warp - kXentEpiWarp;
         const int quarter = w & 3, half = w >> 2;    // rows (a warp reaches the tensor memory lanes of its rank modulo 4), columns
         const u32 stage_smem = staging + w * S::kStaging;
