@@ -629,6 +629,7 @@ int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_strid
         set_rounds(pw, L.dw_per, fine);
         pw.part = (float*)(ws + L.off_dw_part);
         pw.ld = dw_stride, pw.out_bf16 = grad_type == TK_BF16;
+        pw.quads = dim % 4 == 0 && dw_stride % 4 == 0 && aligned(dw, 4 * e);
     }
     if (dh) {   // dh[t][:] = sum over the vocabulary of D[t][v] w[v][:]
         rc = make_map(d, &ph.a, ws + L.off_d, 64, tokens, 64, panels * L.d_parts, kTileM);
@@ -641,6 +642,7 @@ int tk_xent_grad(const void* h, int64_t h_stride, const void* w, int64_t w_strid
         ph.acc = (float*)(ws + L.off_acc);
         ph.part = (float*)(ws + L.off_dh_part);
         ph.ld = dh_stride, ph.rows = tokens, ph.out_bf16 = grad_type == TK_BF16;
+        ph.quads = dim % 4 == 0 && dh_stride % 4 == 0 && aligned(dh, 4 * e);
     }
     for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
         const int64_t here = vocab - v0 < L.piece ? vocab - v0 : L.piece;

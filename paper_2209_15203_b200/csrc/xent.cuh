@@ -60,8 +60,7 @@ template <int CG, int MODE> struct XentShape {
     static constexpr int kBRows = kTileN / CG;                // rows of the right operand this CTA holds
     static constexpr int kStageBytes = kABytes + kBRows * kTileK * 2;
     static constexpr int kStages = CG == 1 ? 4 : 6;           // 192 KB (kSoft with 5 stages and larger store buffers: 7 % slower)
-    // per epilogue warp: kSoft 32 x 64 values of D, swizzled; kGrad 32 x 32 values in rows of 33
-    static constexpr int kStaging = MODE == kXentSoft ? 4096 : 4224;
+    static constexpr int kStaging = 4096;                     // per epilogue warp: kSoft 32 x 64 values of D, kGrad 32 x 32 sums, swizzled
     static constexpr int kSmem = kStages * kStageBytes + kXentEpiWarps * kStaging + 512 + 1024;
 };
 
@@ -84,6 +83,7 @@ struct alignas(64) XentProblem {
     float* part;              // splits > 1: [splits][tiles][128 CG][256] sums, joined by xent_join_tiles_kernel
     int64_t ld, rows;
     int out_bf16, acc_read, acc_write;
+    int quads;                // cols, ld and the bases allow accesses of four values
 };
 
 struct XentArgs {
@@ -438,45 +438,51 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                                    : P.part + (((int64_t)t.split * P.tiles_m + t.m) * P.tiles_n + t.n) * kTileM * CG * kTileN +
                                          ((int)rank * kTileM + 32 * quarter) * kTileN + half * kEpiCols;
                 const int64_t pitch = whole ? P.cols : kTileN, ld = P.ld;
-                const bool read = whole && P.acc_read, write = !whole || P.acc_write;
-                void* out = whole ? P.out : nullptr;
+                const bool read = whole && P.acc_read, write = !whole || P.acc_write, quads = !whole || P.quads;
                 const bool out_bf16 = P.out_bf16;
-                if (out) out = (char*)out + ((int64_t)m0 * ld + n0) * (out_bf16 ? 2 : 4);
-                // 32 columns at a time across the warp, so that a row's stores are one line; 16 rows are read back before the
-                // first is stored (one by one, a tile took 25,000 cycles, and fp32 gradients waited for it)
+                char* out = whole ? (char*)P.out : nullptr;
+                if (out) out += ((int64_t)m0 * ld + n0) * (out_bf16 ? 2 : 4);
+                // 32 columns at a time across the warp, four values per lane and access: a tile of 128 x 256 written value by
+                // value took 20,000 cycles (22 instructions a value), which is what products over few tokens waited for
 #pragma unroll
                 for (int c = 0; c < kEpiCols; c += 32) {
                     __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) stage_ptr[lane * 33 + i] = v[c + i];
+                    for (int j = 0; j < 8; ++j)
+                        *(float4*)(stage_ptr + lane * 32 + ((j ^ (lane & 7)) << 2)) =
+                            make_float4(v[c + 4 * j], v[c + 4 * j + 1], v[c + 4 * j + 2], v[c + 4 * j + 3]);
                     __syncwarp();
-                    if (c + lane < cols) {
-#pragma unroll 1
-                        for (int r0 = 0; r0 < rows; r0 += 16) {
-                            float x[16];
+                    const int g = lane & 7, col = c + 4 * g;
+                    if (col < cols) {
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) x[r] = stage_ptr[(r0 + r) * 33 + lane];
-                            float* to = sum + r0 * pitch + c + lane;
-                            if (read) {
+                        for (int k = 0; k < 8; ++k) {
+                            const int r = 4 * k + (lane >> 3);
+                            float4 x = *(const float4*)(stage_ptr + r * 32 + ((g ^ (r & 7)) << 2));
+                            if (r >= rows) continue;
+                            float* to = sum + r * pitch + col;
+                            const int64_t at = r * ld + col;
+                            if (quads) {
+                                if (read) {
+                                    const float4 q = *(const float4*)to;
+                                    x = make_float4(x.x + q.x, x.y + q.y, x.z + q.z, x.w + q.w);
+                                }
+                                if (write) *(float4*)to = x;
+                                if (out && out_bf16) {
+                                    __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
+                                    *(uint2*)((bf16*)out + at) = make_uint2(*(u32*)&lo, *(u32*)&hi);
+                                } else if (out) {
+                                    *(float4*)((float*)out + at) = x;
+                                }
+                            } else {
+                                const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                                for (int r = 0; r < 16; ++r)
-                                    if (r0 + r < rows) x[r] += to[r * pitch];
-                            }
-                            if (write) {
-#pragma unroll
-                                for (int r = 0; r < 16; ++r)
-                                    if (r0 + r < rows) to[r * pitch] = x[r];
-                            }
-                            if (out && out_bf16) {
-                                bf16* o = (bf16*)out + r0 * ld + c + lane;
-#pragma unroll
-                                for (int r = 0; r < 16; ++r)
-                                    if (r0 + r < rows) o[r * ld] = from_float<bf16>(x[r]);
-                            } else if (out) {
-                                float* o = (float*)out + r0 * ld + c + lane;
-#pragma unroll
-                                for (int r = 0; r < 16; ++r)
-                                    if (r0 + r < rows) o[r * ld] = x[r];
+                                for (int i = 0; i < 4; ++i) {
+                                    if (col + i >= cols) break;
+                                    float z = y[i];
+                                    if (read) z += to[i];
+                                    if (write) to[i] = z;
+                                    if (out) store_any(out, at + i, z, out_bf16);
+                                }
                             }
                         }
                     }
