@@ -444,48 +444,55 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                 if (out) out += ((int64_t)m0 * ld + n0) * (out_bf16 ? 2 : 4);
                 // 32 columns at a time across the warp, four values per lane and access: a tile of 128 x 256 written value by
                 // value took 20,000 cycles (22 instructions a value), which is what products over few tokens waited for
+                auto scatter = [&](auto put) {
 #pragma unroll
-                for (int c = 0; c < kEpiCols; c += 32) {
-                    __syncwarp();
+                    for (int c = 0; c < kEpiCols; c += 32) {
+                        __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *(float4*)(stage_ptr + lane * 32 + ((j ^ (lane & 7)) << 2)) =
-                            make_float4(v[c + 4 * j], v[c + 4 * j + 1], v[c + 4 * j + 2], v[c + 4 * j + 3]);
-                    __syncwarp();
-                    const int g = lane & 7, col = c + 4 * g;
-                    if (col < cols) {
+                        for (int j = 0; j < 8; ++j)
+                            *(float4*)(stage_ptr + lane * 32 + ((j ^ (lane & 7)) << 2)) =
+                                make_float4(v[c + 4 * j], v[c + 4 * j + 1], v[c + 4 * j + 2], v[c + 4 * j + 3]);
+                        __syncwarp();
+                        const int g = lane & 7, col = c + 4 * g;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int r = 4 * k + (lane >> 3);
-                            float4 x = *(const float4*)(stage_ptr + r * 32 + ((g ^ (r & 7)) << 2));
-                            if (r >= rows) continue;
-                            float* to = sum + r * pitch + col;
-                            const int64_t at = r * ld + col;
-                            if (quads) {
-                                if (read) {
-                                    const float4 q = *(const float4*)to;
-                                    x = make_float4(x.x + q.x, x.y + q.y, x.z + q.z, x.w + q.w);
-                                }
-                                if (write) *(float4*)to = x;
-                                if (out && out_bf16) {
-                                    __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
-                                    *(uint2*)((bf16*)out + at) = make_uint2(*(u32*)&lo, *(u32*)&hi);
-                                } else if (out) {
-                                    *(float4*)((float*)out + at) = x;
-                                }
-                            } else {
-                                const float y[4] = {x.x, x.y, x.z, x.w};
+                        for (int half_rows = 0; half_rows < 32; half_rows += 16) {
+                            float4 x[4];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    if (col + i >= cols) break;
-                                    float z = y[i];
-                                    if (read) z += to[i];
-                                    if (write) to[i] = z;
-                                    if (out) store_any(out, at + i, z, out_bf16);
-                                }
+                            for (int k = 0; k < 4; ++k) {
+                                const int r = half_rows + 4 * k + (lane >> 3);
+                                x[k] = *(const float4*)(stage_ptr + r * 32 + ((g ^ (r & 7)) << 2));
+                            }
+                            if (col < cols) {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (half_rows + 4 * k + (lane >> 3) < rows) put(half_rows + 4 * k + (lane >> 3), col, x[k]);
                             }
                         }
                     }
+                };
+                if (quads && write && !read && !out) {
+                    scatter([&](int r, int col, float4 x) { *(float4*)(sum + r * pitch + col) = x; });
+                } else if (quads && out && !read && !write && out_bf16) {
+                    scatter([&](int r, int col, float4 x) {
+                        __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
+                        *(uint2*)((bf16*)out + r * ld + col) = make_uint2(*(u32*)&lo, *(u32*)&hi);
+                    });
+                } else if (quads && out && !read && !write) {
+                    scatter([&](int r, int col, float4 x) { *(float4*)((float*)out + r * ld + col) = x; });
+                } else {
+                    scatter([&](int r, int col, float4 x) {
+                        const float y[4] = {x.x, x.y, x.z, x.w};
+                        float* to = sum + r * pitch + col;
+                        const int64_t at = r * ld + col;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (col + i >= cols) break;
+                            float z = y[i];
+                            if (read) z += to[i];
+                            if (write) to[i] = z;
+                            if (out) store_any(out, at + i, z, out_bf16);
+                        }
+                    });
                 }
             }
         }
