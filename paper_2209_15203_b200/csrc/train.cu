@@ -283,7 +283,7 @@ int xent_pairs(int parts_a, int parts_b) { return parts_a == 1 || parts_b == 1 ?
 // what an item costs beside its rounds, a launch, and the bytes that a join moves meanwhile.  All splits and a few
 // numbers of pieces are tried (about 5 us of host time).
 constexpr int kXentSms = 148;        // a wrong guess costs speed, nothing else: results do not change with the device
-constexpr int kMaxSplits = 32, kMorePieces = 6;
+constexpr int kMaxSplits = 148, kMorePieces = 6;
 constexpr double kItemCost = 8.0, kWholeCost = 4.0, kSoftCost = 3.0, kLaunchCost = 10.0, kRoundBytes = 1.7e6;
 constexpr size_t kPartBytes = (size_t)256 << 20;   // at most, per product
 
@@ -319,11 +319,11 @@ XentPlan xent_plan(int64_t tokens, int64_t vocab, int64_t dim, int in_parts, int
         const int64_t dh_rounds = ceil_div(piece < vocab ? piece : vocab, kTileK) * pairs, dw_rounds = ceil_div(tokens, kTileK) * pairs;
         const double soft = (double)ceil_div(tiles_m * piece_tiles, workers) * (soft_rounds + kSoftCost) + 2 * kLaunchCost;
         const double sums = count > 1 ? 8.0 * tokens * dim : 0.0;
-        for (int sh = 1; sh <= kMaxSplits; ++sh) {
+        for (int sh = 1; sh <= kMaxSplits; sh += 1 + sh / 12) {   // every number up to 12, then ever wider steps
             if (sh > 1 && (dh_rounds < 8 * sh || sh * dh_tiles * tile_bytes > kPartBytes || dh_tiles * sh > 16 * workers)) break;
             const int64_t ph = ceil_div(dh_rounds, sh), nh = dh_tiles * ceil_div(dh_rounds, ph);
             const double join_h = sh > 1 ? (nh * tile_bytes + sums) * size / kRoundBytes + kLaunchCost : 0.0;
-            for (int sw = 1; sw <= kMaxSplits; ++sw) {
+            for (int sw = 1; sw <= kMaxSplits; sw += 1 + sw / 12) {
                 if (sw > 1 && (dw_rounds < 8 * sw || sw * dw_tiles * tile_bytes > kPartBytes || dw_tiles * sw > 16 * workers)) break;
                 const int64_t pw = ceil_div(dw_rounds, sw), nw = dw_tiles * ceil_div(dw_rounds, pw);
                 const double join_w = sw > 1 ? nw * tile_bytes * size / kRoundBytes + kLaunchCost : 0.0;

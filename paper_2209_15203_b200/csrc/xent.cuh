@@ -433,12 +433,12 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                     }
             } else {
                 const bool whole = P.splits == 1;
-                const int cols = whole ? P.cols - n0 : kEpiCols, rows = whole ? (int)min((int64_t)32, P.rows - m0) : 32;
+                const int cols = P.cols - n0, rows = (int)min((int64_t)32, P.rows - m0);   // of a cut tile too: nothing reads the rest
                 float* sum = whole ? P.acc + (int64_t)m0 * P.cols + n0
                                    : P.part + (((int64_t)t.split * P.tiles_m + t.m) * P.tiles_n + t.n) * kTileM * CG * kTileN +
                                          ((int)rank * kTileM + 32 * quarter) * kTileN + half * kEpiCols;
                 const int64_t pitch = whole ? P.cols : kTileN, ld = P.ld;
-                const bool read = whole && P.acc_read, write = !whole || P.acc_write, quads = !whole || P.quads;
+                const bool read = whole && P.acc_read, write = !whole || P.acc_write, quads = P.quads || (!whole && P.cols % 4 == 0);
                 const bool out_bf16 = P.out_bf16;
                 char* out = whole ? (char*)P.out : nullptr;
                 if (out) out += ((int64_t)m0 * ld + n0) * (out_bf16 ? 2 : 4);
@@ -479,20 +479,54 @@ __global__ void __launch_bounds__(kXentThreads, 1) xent_kernel(const __grid_cons
                     });
                 } else if (quads && out && !read && !write) {
                     scatter([&](int r, int col, float4 x) { *(float4*)((float*)out + r * ld + col) = x; });
-                } else {
+                } else if (quads) {   // the sum over the pieces is read or written as well
                     scatter([&](int r, int col, float4 x) {
-                        const float y[4] = {x.x, x.y, x.z, x.w};
                         float* to = sum + r * pitch + col;
+                        if (read) {
+                            const float4 q = *(const float4*)to;
+                            x = make_float4(x.x + q.x, x.y + q.y, x.z + q.z, x.w + q.w);
+                        }
+                        if (write) *(float4*)to = x;
+                        if (!out) return;
                         const int64_t at = r * ld + col;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (col + i >= cols) break;
-                            float z = y[i];
-                            if (read) z += to[i];
-                            if (write) to[i] = z;
-                            if (out) store_any(out, at + i, z, out_bf16);
+                        if (out_bf16) {
+                            __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
+                            *(uint2*)((bf16*)out + at) = make_uint2(*(u32*)&lo, *(u32*)&hi);
+                        } else {
+                            *(float4*)((float*)out + at) = x;
                         }
                     });
+                } else {
+                    // rows off the 16-byte grid (slices of a gradient row, odd widths): a column per lane, one row per access
+#pragma unroll 1
+                    for (int c = 0; c < kEpiCols; c += 32) {
+                        __syncwarp();
+#pragma unroll
+                        for (int cc = 0; cc < kEpiCols; cc += 32)
+                            if (cc == c) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    *(float4*)(stage_ptr + lane * 32 + ((j ^ (lane & 7)) << 2)) =
+                                        make_float4(v[cc + 4 * j], v[cc + 4 * j + 1], v[cc + 4 * j + 2], v[cc + 4 * j + 3]);
+                            }
+                        __syncwarp();
+                        if (c + lane >= cols) continue;
+                        float* to = sum + c + lane;
+                        int64_t at = c + lane;
+#pragma unroll 1
+                        for (int r0 = 0; r0 < rows; r0 += 8) {
+                            float x[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) x[k] = stage_ptr[(r0 + k) * 32 + (((lane >> 2) ^ k) << 2) + (lane & 3)];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k, to += pitch, at += ld)
+                                if (r0 + k < rows) {
+                                    if (read) x[k] += *to;
+                                    if (write) *to = x[k];
+                                    if (out) store_any(out, at, x[k], out_bf16);
+                                }
+                        }
+                    }
                 }
             }
         }
