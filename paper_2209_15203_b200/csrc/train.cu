@@ -501,7 +501,7 @@ template <typename T, int PARTS>
 int launch_pack(Device* d, const XentLayout& L, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int64_t tokens,
                 int64_t vocab, int64_t dim, char* ws, cudaStream_t s) {
     const PackInput<T> first = {(const T*)h, h_stride, tokens, (bf16*)(ws + L.off_h)}, second = {(const T*)w, w_stride, vocab, (bf16*)(ws + L.off_w)};
-    const int64_t ctas = ceil_div(tokens + vocab, 8), most = (int64_t)d->sms * 8;
+    const int64_t ctas = ceil_div((tokens + vocab) * (L.ld / 8), 256), most = (int64_t)d->sms * 16;
     return launch_after(xent_pack_kernel<T, PARTS>, dim3((unsigned)(ctas < most ? ctas : most)), 256, s, first, second, (int)dim, L.ld);
 }
 int xent_inputs(Device* d, const XentLayout& L, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int in_type,

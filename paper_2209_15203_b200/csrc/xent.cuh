@@ -617,8 +617,8 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2* partial, c
     }
 }
 
-// An operand [rows][dim] as PARTS bf16 matrices [rows][ld] (zeros beyond dim; ld is a multiple of 8): one warp per row and 256
-// columns, eight neighbouring ones per thread; ahead of that the second operand's rows, if there is one.
+// Operands [rows][dim] as PARTS bf16 matrices [rows][ld] each (zeros beyond dim; ld is a multiple of 8): a thread takes eight
+// neighbouring columns of a row of the first operand or, after those, of the second.
 template <typename T> struct PackInput {
     const T* x;
     int64_t stride, rows;
@@ -627,26 +627,26 @@ template <typename T> struct PackInput {
 template <typename T, int PARTS>
 __global__ void __launch_bounds__(256) xent_pack_kernel(const PackInput<T> first, const PackInput<T> second, int dim, int ld) {
     wait_for_predecessor();
-    const int64_t warps = (int64_t)gridDim.x * 8;
-    const int lane = threadIdx.x & 31;
-    for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < first.rows + second.rows; row += warps) {
+    const u32 groups = (u32)ld / 8;
+    const int64_t n = (first.rows + second.rows) * groups, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+        const int64_t row = n <= 0xffffffffll ? (int64_t)((u32)i / groups) : i / groups;
+        const int c = (int)(i - row * groups) * 8;
         const bool one = row < first.rows;
         const int64_t r = one ? row : row - first.rows, rows = one ? first.rows : second.rows;
-        const T* x = (one ? first.x : second.x) + r * (one ? first.stride : second.stride);
-        bf16* out = (one ? first.out : second.out) + r * ld;
-        for (int c = lane * 8; c < ld; c += 256) {
-            float v[8];
+        const T* x = (one ? first.x : second.x) + r * (one ? first.stride : second.stride) + c;
+        bf16* out = (one ? first.out : second.out) + r * ld + c;
+        float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? to_float(x[c + i]) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[j] = c + j < dim ? to_float(x[j]) : 0.0f;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                uint4 q;
-                q.x = take_part(v[0], v[1], p == PARTS - 1);
-                q.y = take_part(v[2], v[3], p == PARTS - 1);
-                q.z = take_part(v[4], v[5], p == PARTS - 1);
-                q.w = take_part(v[6], v[7], p == PARTS - 1);
-                *(uint4*)(out + p * rows * ld + c) = q;
-            }
+        for (int p = 0; p < PARTS; ++p) {
+            uint4 q;
+            q.x = take_part(v[0], v[1], p == PARTS - 1);
+            q.y = take_part(v[2], v[3], p == PARTS - 1);
+            q.z = take_part(v[4], v[5], p == PARTS - 1);
+            q.w = take_part(v[6], v[7], p == PARTS - 1);
+            *(uint4*)(out + p * rows * ld) = q;
         }
     }
 }
