@@ -31,9 +31,9 @@
 // instructions take such operands ("MN-major") directly, so nothing is transposed in memory.
 //
 // Bound by the matrix pipe, and in long runs by the power limit behind it; for few tokens by reading w.  Measured on one B200
-// (bf16): 4096 tokens x 131,072 x 2048, loss 1332 us (1652 TFLOP/s, matrix pipe active 94 % of the cycles), a piece's D
+// (bf16): 4096 tokens x 131,072 x 2048, loss 1332 us (1652 TFLOP/s, matrix pipe active 96 % of the cycles), a piece's D
 // 333 us, its two products 718 us; loss and gradient together 5.74 ms alone, 6.66 ms back to back at the power limit (1322 TFLOP/s of
-// the 8 flops per token, entry and dim).  8192 x 50,257 x 768: loss 406 us, D 5 x 93 us, products 5 x 175 us.  61 tokens x 50,257 x 768: 22 us
+// the 8 flops per token, entry and dim).  8192 x 50,257 x 768: loss 406 us, D 5 x 93 us, products 5 x 173 us.  61 tokens x 50,257 x 768: 22 us
 // (3.5 TB/s of w; the second round of tiles fills a third of the SMs).
 #pragma once
 
