@@ -472,6 +472,7 @@ int tk_xent_status(void);
  * One AdamW step over many tensors (decoupled weight decay, bias-corrected moments):
  *   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2          g = grad_scale * gradient
  *   p <- p - lr weight_decay p - lr / (1 - b1^step) * m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * (a second moment below the smallest normal number counts as zero in the step's root).
  * One launch serves up to 500 tensors.  The arrays `tensors` and `grads` are host memory and may be
  * reused as soon as the call returns.
  *   n             values of the tensor, >= 0
